@@ -399,6 +399,105 @@ int gk_fingerprints(gk_ctx *ctx, const void *data_dev, const uint64_t *offsets_d
 int gk_blob_digests(gk_ctx *ctx, const gk_job *jobs, uint32_t n_jobs, const uint8_t *keys_dev,
                     uint8_t *digests_dev, uint8_t *page_digests_dev, void *stream);
 
+/* Using the cache: appending new tokens to it and attending over it.  (The paper leaves both to the
+ * runtime that it wraps; here they close the loop: a restored block is followed by the question's
+ * tokens, and every layer of every step writes its new keys and values behind the restored ones and
+ * attends over both, through the page tables that gk_restore filled.)  One call works on one layer.
+ *
+ * gk_batch describes the sequences of a call.  Sequence s has the rows q_start[s] .. q_start[s+1]-1
+ * of the call's token tensors; q_start == NULL means one token for every sequence (n_tokens ==
+ * n_seqs).  kv_len[s] counts the tokens of the sequence in the cache INCLUDING those new ones, so
+ * that its row i is the token at position kv_len[s] - q_len[s] + (i - q_start[s]), in the page
+ * page_table[s * table_stride + position / page_tokens].  A sequence may have no new token
+ * (q_len = 0) or an empty cache (kv_len = 0).  The lengths and tables are read on the device, so a
+ * captured call follows them as they change; n_tokens, n_seqs and max_q_len are the host's:
+ * q_start[n_seqs] must be n_tokens and no sequence may have more than max_q_len rows (max_q_len only
+ * chooses between kernels; 0 stands for n_tokens).  Rows at negative positions (kv_len < q_len) are
+ * not appended and attend to nothing.
+ *
+ * status (device, n_seqs bytes, may be NULL) is only ever raised: the caller clears it once and
+ * finds a code there after any call that met a fault in that sequence.  GK_JOB_PAGE_TABLE: an id
+ * outside [0, num_pages), or kv_len larger than max_pages * page_tokens.  Fail closed: what such a
+ * page should have held is not written, and every row that would have had to read it comes out as
+ * NaN.  GK_SEQ_POSITION: a rotation index outside [0, max_pos); the token's query and key rows are
+ * NaN. */
+#define GK_SEQ_POSITION 5u
+
+typedef struct {
+    const int32_t *page_table; /* device: n_seqs rows of max_pages page ids */
+    uint64_t table_stride;     /* entries from one row to the next */
+    const int32_t *q_start;    /* device: n_seqs + 1, ascending from 0, or NULL */
+    const int32_t *kv_len;     /* device: n_seqs */
+    uint8_t *status;           /* device: n_seqs, or NULL */
+    uint32_t n_seqs, n_tokens;
+    uint32_t max_pages, max_q_len;
+} gk_batch;
+
+/* bf16 rows [token][head][head_dim], head_dim contiguous; strides in elements, multiples of 8; data
+ * 16-byte aligned.  q, k and v may be slices of one projection's output. */
+typedef struct {
+    void *data; /* device */
+    uint64_t token_stride, head_stride;
+} gk_rows;
+
+/* Rotary positions.  cos_sin is a table of max_pos rows of rotary_dim fp32 values, rotary_dim/2
+ * cosines and then as many sines (device, 16-byte aligned); rotary_dim is a multiple of 16, at most
+ * head_dim; the dimensions from rotary_dim on are not rotated.  Pair i of a head is the dimensions
+ * (i, i + rotary_dim/2), or with interleaved = 1 (2i, 2i + 1).  axes = 1, 2 or 3 (e.g. time, height,
+ * width of image and video tokens): the first section[0] pairs turn by the position on axis 0, the next
+ * section[1] by that on axis 1, and so on; the sections sum to rotary_dim/2.  positions: device int32,
+ * [axes][n_tokens]; NULL (axes = 1 only) takes the token's position in its sequence.
+ * A pair (a, b) becomes (a*c - b*s, b*c + a*s), in fp32 with every product rounded by itself. */
+typedef struct {
+    const float *cos_sin;
+    const int32_t *positions;
+    uint32_t max_pos, rotary_dim;
+    uint32_t interleaved, axes;
+    uint32_t section[3];
+    uint32_t reserved; /* must be 0 */
+} gk_rope;
+
+/* Appends the new keys and values of one layer to the cache, rotating keys (and, if q is not NULL,
+ * queries into q_out, which may be q itself) on the way.  rope == NULL: nothing is rotated.  v is never
+ * rotated.  Rows of a page behind the last appended token keep their bytes, and so does every page
+ * that the call does not append to.  Two sequences of one call must not append to the same page.
+ *
+ * bf16 caches: key and value rows are rounded to bf16 once, after the rotation.
+ * fp8 caches: per page, head and K/V (K and V together with scale_kv == 1), A = the largest finite
+ * |value| that the call appends to the page, s0 = the page's scale if the page holds earlier tokens of
+ * the sequence and that scale is positive and finite, else 1.  The new scale is s0 * 2^k with the
+ * least k for which A / (448 * s0) <= 2^k, and k >= 0 if s0 was the page's (a page's scale only
+ * grows while it fills); k = 0 if A is 0.  Earlier tokens of a page whose scale has grown are rescaled
+ * by 2^-k, which is exact but for the smallest values, so that a page filled token by token does not wear
+ * out.  Values are stored as the nearest e4m3 of value / scale; infinities and NaN as NaN.
+ *
+ * head_dim must be a multiple of 16 and at most 256 (else GK_ERR_UNSUPPORTED).  One launch; no
+ * synchronisation or copy; may be captured.  n_tokens == 0 is a no-op. */
+int gk_append(gk_ctx *ctx, const gk_cache *dst, uint32_t layer, const gk_batch *batch, const gk_rope *rope,
+              const gk_rows *k, const gk_rows *v, uint32_t q_heads, const gk_rows *q, const gk_rows *q_out,
+              void *stream);
+
+/* Attention of the call's rows over the cache of one layer (the new tokens' own keys and values
+ * included: append them first).  q_heads is a multiple of kv_heads; query head h reads key head
+ * h / (q_heads / kv_heads).  For the row at position p of a sequence with n = kv_len tokens
+ *     out = sum_t w_t V_t / sum_t w_t,   w_t = exp(scale * (q . K_t) - max),
+ * over the tokens 0 <= t < n with t <= p (unless GK_ATTN_FULL is set) and, with window > 0,
+ * t > p - window.  An fp8 cache's K and V are its values times the scale of their page and head.
+ * A row with no token to attend to gives zeros.  lse (device fp32 [n_tokens][q_heads], may be NULL)
+ * receives log(sum_t exp(scale * (q . K_t))), -infinity for such a row: two results over different
+ * tokens can be joined with it.  Only tokens that a row attends to reach its result, whatever the others
+ * hold (infinities and NaN included).
+ *
+ * Scores, maxima, sums and outputs are accumulated in fp32; the bf16 result is rounded once.
+ * The work is split along the cache among the whole GPU whatever the lengths; partial results are joined in a
+ * fixed order, so a call with the same arguments gives the same bits.  Needs head_dim a multiple of 16 up
+ * to 256 (else GK_ERR_UNSUPPORTED).  The first call of a context allocates its workspace (gk_stats.allocations; a call
+ * with n_tokens == 0 does that and nothing else); later ones allocate nothing and may be captured.  */
+#define GK_ATTN_FULL 1u
+int gk_attention(gk_ctx *ctx, const gk_cache *cache, uint32_t layer, const gk_batch *batch, uint32_t q_heads,
+                 const gk_rows *q, const gk_rows *out, float *lse, float scale, uint32_t window, uint32_t flags,
+                 void *stream);
+
 /* Bounds-checked build.  Section 3's sabotage paragraph reports that an address
  * sanitizer found the one out-of-bounds read of the paper's own code; a GPU
  * library cannot lean on such a tool everywhere, so this one can be compiled

@@ -19,18 +19,21 @@ _HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.environ.get("GK_LIB_PATH") or os.path.join(_HERE, "libgk.so")
 
 GK_OK = 0
+GK_ERR_ARG = -1
 GK_BF16, GK_FP8_E4M3 = 0, 1
 GK_FLAG_SKIP_VERIFY = 1
 GK_FLAG_HEAD_MAJOR = 2
 GK_FLAG_SINGLE_PASS = 4
+GK_ATTN_FULL = 1
 JOB_OK, JOB_CHECKSUM, JOB_PAGE_TABLE, JOB_MISSING, JOB_TIMEOUT = 0, 1, 2, 3, 4
+SEQ_POSITION = 5
 
 EXPORTS = ["gk_blob_size", "gk_ctx_create", "gk_ctx_destroy", "gk_last_error", "gk_pack_batch", "gk_pack",
            "gk_page_checksums", "gk_restore", "gk_restore_host", "gk_get_stats", "gk_ctx_set_tuning", "gk_get_kernel_times",
            "gk_page_checksums_noalloc", "gk_pack_host", "gk_verify", "gk_commit", "gk_restore_stream",
            "gk_fingerprints", "gk_blob_digests", "gk_pack_layerwise", "gk_pack_layerwise_host",
            "gk_restore_layerwise", "gk_restore_layerwise_host", "gk_ctx_reserve", "gk_ctx_clear_error",
-           "gk_debug_status", "gk_debug_range_ok", "gk_measure_logic_rate"]
+           "gk_debug_status", "gk_debug_range_ok", "gk_measure_logic_rate", "gk_append", "gk_attention"]
 
 
 class GkError(RuntimeError):
@@ -63,6 +66,22 @@ class CStats(ctypes.Structure):
                 ("bytes_blob", ctypes.c_uint64), ("kernels_launched", ctypes.c_uint64),
                 ("device_wait_expired", ctypes.c_uint32), ("allocations", ctypes.c_uint32),
                 ("calls_restore_stream", ctypes.c_uint64), ("quartet_launches", ctypes.c_uint64)]
+
+
+class CBatch(ctypes.Structure):
+    _fields_ = [("page_table", ctypes.c_void_p), ("table_stride", ctypes.c_uint64), ("q_start", ctypes.c_void_p),
+                ("kv_len", ctypes.c_void_p), ("status", ctypes.c_void_p), ("n_seqs", ctypes.c_uint32),
+                ("n_tokens", ctypes.c_uint32), ("max_pages", ctypes.c_uint32), ("max_q_len", ctypes.c_uint32)]
+
+
+class CRows(ctypes.Structure):
+    _fields_ = [("data", ctypes.c_void_p), ("token_stride", ctypes.c_uint64), ("head_stride", ctypes.c_uint64)]
+
+
+class CRope(ctypes.Structure):
+    _fields_ = [("cos_sin", ctypes.c_void_p), ("positions", ctypes.c_void_p), ("max_pos", ctypes.c_uint32),
+                ("rotary_dim", ctypes.c_uint32), ("interleaved", ctypes.c_uint32), ("axes", ctypes.c_uint32),
+                ("section", ctypes.c_uint32 * 3), ("reserved", ctypes.c_uint32)]
 
 
 class CWindowBlock(ctypes.Structure):
@@ -174,6 +193,13 @@ def load_library() -> ctypes.CDLL:
     L.gk_ctx_clear_error.argtypes = [vp, vp]
     L.gk_measure_logic_rate.restype = ctypes.c_int
     L.gk_measure_logic_rate.argtypes = [vp, ctypes.POINTER(ctypes.c_double), vp]
+    rows = ctypes.POINTER(CRows)
+    L.gk_append.restype = ctypes.c_int
+    L.gk_append.argtypes = [vp, ctypes.POINTER(CCache), u32, ctypes.POINTER(CBatch), ctypes.POINTER(CRope), rows, rows,
+                            u32, rows, rows, vp]
+    L.gk_attention.restype = ctypes.c_int
+    L.gk_attention.argtypes = [vp, ctypes.POINTER(CCache), u32, ctypes.POINTER(CBatch), u32, rows, rows, vp,
+                               ctypes.c_float, u32, u32, vp]
     L.gk_debug_status.restype = ctypes.c_int
     L.gk_debug_status.argtypes = [vp, ctypes.POINTER(ctypes.c_uint32)]
     L.gk_debug_range_ok.restype = ctypes.c_int
@@ -214,6 +240,73 @@ class Cache:
         return CCache(self.data.data_ptr(), self.num_pages, self.layer_stride, self.kv_stride, self.page_stride,
                       0 if self.scales is None else self.scales.data_ptr(), self.s_layer_stride,
                       self.s_kv_stride, self.s_page_stride)
+
+
+class Batch:
+    """The sequences of a gk_append or gk_attention call (gk_batch in gk.h).
+
+    page_table: int32 [n_seqs, max_pages]; kv_len: int32 [n_seqs], tokens in the cache with the new ones;
+    q_start: int32 [n_seqs + 1] row offsets, or None for one token per sequence; n_tokens: rows of the token
+    tensors (the last entry of q_start, which stays on the device); max_q_len: the most rows that a
+    sequence has; status: uint8 [n_seqs], raised where a sequence meets a fault.  All on the device; the
+    tensors' contents may change between calls, the tensors themselves are this object's.
+    """
+
+    def __init__(self, page_table: torch.Tensor, kv_len: torch.Tensor, q_start: Optional[torch.Tensor] = None,
+                 n_tokens: Optional[int] = None, max_q_len: Optional[int] = None, status: Optional[torch.Tensor] = None):
+        n = kv_len.numel()
+        _need(page_table.dtype == torch.int32 and page_table.dim() == 2 and page_table.shape[0] == n and
+              (page_table.stride(1) == 1 or page_table.shape[1] <= 1), "page_table: int32 [n_seqs, max_pages], rows contiguous")
+        _need(kv_len.dtype == torch.int32 and kv_len.dim() == 1 and kv_len.is_contiguous(), "kv_len: int32 [n_seqs]")
+        if q_start is None:
+            _need(n_tokens is None or n_tokens == n, "without q_start every sequence has one token")
+            n_tokens, max_q_len = n, 1
+        else:
+            _need(q_start.dtype == torch.int32 and q_start.numel() == n + 1 and q_start.is_contiguous(),
+                  "q_start: int32 [n_seqs + 1]")
+            _need(n_tokens is not None, "n_tokens is needed with q_start")
+        if status is not None:
+            _need(status.dtype == torch.uint8 and status.numel() >= n and status.is_contiguous(), "status: uint8 [n_seqs]")
+        self.page_table, self.kv_len, self.q_start, self.status = page_table, kv_len, q_start, status
+        self.n_seqs, self.n_tokens, self.max_q_len = n, int(n_tokens), int(max_q_len or n_tokens)
+        self._c = CBatch(_ptr(page_table), page_table.stride(0), _ptr(q_start), _ptr(kv_len), _ptr(status), n,
+                         self.n_tokens, page_table.shape[1], self.max_q_len)
+        self._ref = ctypes.byref(self._c)
+
+
+class Rope:
+    """Rotary positions of gk_append (gk_rope in gk.h): cos_sin float32 [max_pos, rotary_dim], the cosines and then
+    the sines of a position; sections: how many pairs turn by each axis; positions: int32 [axes, n_tokens]."""
+
+    def __init__(self, cos_sin: torch.Tensor, interleaved: bool = False, sections: Optional[Sequence[int]] = None,
+                 positions: Optional[torch.Tensor] = None):
+        _need(cos_sin.dtype == torch.float32 and cos_sin.dim() == 2 and cos_sin.is_contiguous(),
+              "cos_sin: contiguous float32 [max_pos, rotary_dim]")
+        sections = tuple(sections) if sections is not None else (cos_sin.shape[1] // 2,)
+        _need(1 <= len(sections) <= 3, "one to three axes")
+        if positions is not None:
+            _need(positions.dtype == torch.int32 and positions.is_contiguous() and
+                  positions.numel() % len(sections) == 0 and (positions.dim() == 1 or positions.shape[0] == len(sections)),
+                  "positions: contiguous int32 [axes, n_tokens]")
+        self.cos_sin, self.positions, self.axes = cos_sin, positions, len(sections)
+        sec = (ctypes.c_uint32 * 3)(*(list(sections) + [0, 0])[:3])
+        self._c = CRope(_ptr(cos_sin), _ptr(positions), cos_sin.shape[0], cos_sin.shape[1], int(interleaved), len(sections),
+                        sec, 0)
+        self._ref = ctypes.byref(self._c)
+
+
+def _need(ok: bool, what: str) -> None:
+    if not ok:
+        raise GkError(GK_ERR_ARG, "arguments", what)
+
+
+def _rows(x: torch.Tensor, n_tokens: int, heads: int, head_dim: int, name: str):
+    """A CRows reference for a bf16 tensor [n_tokens, heads, head_dim]."""
+    if x.dtype != torch.bfloat16 or x.dim() != 3 or x.shape[0] != n_tokens or x.shape[1] != heads or x.shape[2] != head_dim:
+        _need(False, f"{name}: bf16 [{n_tokens}, {heads}, {head_dim}] is needed, got {x.dtype} {list(x.shape)}")
+    s = x.stride()
+    _need(s[2] == 1, f"{name}: the last dimension must be contiguous")
+    return ctypes.byref(CRows(x.data_ptr(), s[0], s[1]))
 
 
 @dataclass
@@ -453,6 +546,42 @@ class Context:
                         page_digests: Optional[torch.Tensor] = None, stream=None):
         self._check(self._lib.gk_blob_digests(self._h, self._jobs(jobs), len(jobs), _ptr(keys), _ptr(digests),
                                               _ptr(page_digests), _stream_handle(stream)), "gk_blob_digests")
+
+    def gk_append(self, cache: Cache, layer: int, batch: Batch, k: torch.Tensor, v: torch.Tensor,
+                  q: Optional[torch.Tensor] = None, q_out: Optional[torch.Tensor] = None, rope: Optional[Rope] = None,
+                  stream=None):
+        """Appends k and v (bf16 [n_tokens, kv_heads, head_dim]) of one layer to the cache, k rotated by ``rope``, and
+        writes the rotated q (bf16 [n_tokens, q_heads, head_dim]) to q_out, or over q if that is None."""
+        n, H, D = batch.n_tokens, self.geom.kv_heads, self.geom.head_dim
+        heads, rq, ro = 0, None, None
+        if q is not None:
+            heads = q.shape[1] if q.dim() == 3 else 0
+            rq = _rows(q, n, heads, D, "q")
+            ro = rq if q_out is None else _rows(q_out, n, heads, D, "q_out")
+        if rope is not None and rope.positions is not None:
+            _need(rope.positions.numel() == rope.axes * n, "positions: one per axis and token")
+        cc = cache.c()
+        rc = self._lib.gk_append(self._h, ctypes.byref(cc), layer, batch._ref, None if rope is None else rope._ref,
+                                 _rows(k, n, H, D, "k"), _rows(v, n, H, D, "v"), heads, rq, ro, _stream_handle(stream))
+        if rc != GK_OK:
+            self._check(rc, "gk_append")
+
+    def gk_attention(self, cache: Cache, layer: int, batch: Batch, q: torch.Tensor, out: torch.Tensor,
+                     lse: Optional[torch.Tensor] = None, scale: Optional[float] = None, window: int = 0,
+                     causal: bool = True, stream=None):
+        """Attention of q (bf16 [n_tokens, q_heads, head_dim]) over one layer of the cache into out (like q); lse:
+        float32 [n_tokens, q_heads].  scale: 1 / sqrt(head_dim) by default.  window: 0 = the whole sequence."""
+        n, D = batch.n_tokens, self.geom.head_dim
+        heads = q.shape[1] if q.dim() == 3 else 0
+        if lse is not None:
+            _need(lse.dtype == torch.float32 and lse.is_contiguous() and tuple(lse.shape) == (n, heads),
+                  "lse: contiguous float32 [n_tokens, q_heads]")
+        cc = cache.c()
+        rc = self._lib.gk_attention(self._h, ctypes.byref(cc), layer, batch._ref, heads, _rows(q, n, heads, D, "q"),
+                                    _rows(out, n, heads, D, "out"), _ptr(lse), D ** -0.5 if scale is None else scale,
+                                    window, 0 if causal else GK_ATTN_FULL, _stream_handle(stream))
+        if rc != GK_OK:
+            self._check(rc, "gk_attention")
 
     def gk_measure_logic_rate(self, stream=None) -> float:
         """Three-input logic operations per second (lanes x instructions) of this GPU, measured."""

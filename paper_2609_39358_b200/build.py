@@ -4,14 +4,17 @@ from __future__ import annotations
 import os
 import subprocess
 import sys
+import tempfile
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
 _CSRC = os.path.join(_HERE, "csrc")
 LIB_PATH = os.path.join(_HERE, "libgk.so")
 DEBUG_LIB_PATH = os.path.join(_HERE, "libgk_debug.so")   # the bounds-checked build (-DGK_DEBUG)
 
-_SOURCES = ["gk_api.cu"]
-_DEPS = ["gk_api.cu", "gk_kernels.cuh", "gk_device.cuh", "gk_sha256.cuh", "gk_gf2_generated.inc", "gen_tables.py",
+# Every file by itself, then one link.  --use_fast_math is for the integer kernels of gk_api.cu only: the operators on
+# the cache state each approximation where they make it.
+_SOURCES = {"gk_api.cu": ["--use_fast_math"], "gk_ops.cu": []}
+_DEPS = ["gk_api.cu", "gk_ops.cu", "gk_ctx.cuh", "gk_seq.cuh", "gk_append.cuh", "gk_attend.cuh", "gk_kernels.cuh", "gk_device.cuh", "gk_sha256.cuh", "gk_gf2_generated.inc", "gen_tables.py",
          os.path.join("..", "..", "include", "gk.h")]
 
 
@@ -40,17 +43,25 @@ def build(force: bool = False, verbose: bool = False, extra_flags: list[str] | N
     if not force and os.path.exists(lib_path) and os.path.getmtime(lib_path) >= newest:
         return lib_path
     tmp = lib_path + f".tmp{os.getpid()}"
-    cmd = [_nvcc(), "-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17",
-           "-shared", "-Xcompiler", "-fPIC", "-Xcompiler", "-Wall", "--use_fast_math",
-           "-I", os.path.join(_HERE, "..", "include")]
+    base = [_nvcc(), "-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17",
+            "-Xcompiler", "-fPIC", "-Xcompiler", "-Wall", "-I", os.path.join(_HERE, "..", "include")]
     if verbose:
-        cmd += ["-Xptxas", "-v"]
+        base += ["-Xptxas", "-v"]
     if extra_flags:
-        cmd += extra_flags
+        base += extra_flags
     if os.environ.get("GK_NVCC_FLAGS"):
-        cmd += os.environ["GK_NVCC_FLAGS"].split()
-    cmd += [os.path.join(_CSRC, s) for s in _SOURCES] + ["-o", tmp, "-lcudart"]
-    subprocess.check_call(cmd)
+        base += os.environ["GK_NVCC_FLAGS"].split()
+    with tempfile.TemporaryDirectory() as d:
+        objects = [os.path.join(d, s + ".o") for s in _SOURCES]
+        running = [subprocess.Popen(base + flags + ["-c", os.path.join(_CSRC, s), "-o", o])
+                   for (s, flags), o in zip(_SOURCES.items(), objects)]
+        for p in running:
+            p.wait()
+        for p in running:
+            if p.returncode:
+                raise subprocess.CalledProcessError(p.returncode, p.args)
+        subprocess.check_call([_nvcc(), "-gencode", "arch=compute_100a,code=sm_100a", "-shared"] + objects +
+                              ["-o", tmp, "-lcudart"])
     os.replace(tmp, lib_path)
     return lib_path
 

@@ -7,7 +7,6 @@
 
 #include <algorithm>
 #include <cmath>
-#include <cstdarg>
 #include <cstdio>
 #include <cstdlib>
 #include <cstring>
@@ -15,6 +14,7 @@
 #include <new>
 #include <vector>
 
+#include "gk_ctx.cuh"
 #include "gk_kernels.cuh"
 #include "gk_sha256.cuh"
 
@@ -73,8 +73,6 @@ using CommitCfg = StreamCfg<kCommit, 0, GK_COPY_STAGE, GK_COPY_STAGES>;
 using SingleCfg = StreamCfg<kSingle, GK_CRC_NT, GK_PACK_STAGE, GK_PACK_STAGES>;
 using FusedCfg = RestoreCfg<GK_CRC_NT, GK_CRC_STAGE, GK_FUSED_VSTAGES, GK_COPY_STAGE, GK_FUSED_CSTAGES>;
 
-constexpr int kSlots = 2;  // host-tier staging ring
-
 uint64_t gf_xpow(uint64_t n)
 {
     uint64_t r = 1, base = 2;
@@ -96,109 +94,7 @@ uint32_t pages_of(uint32_t n_tokens, uint32_t page_tokens)
 
 }  // namespace
 
-struct gk_ctx {
-    gk_geom geom{};
-    GeomDev gd{};
-    int device = 0;
-    int sm_count = 0;
-    int occ_verify = 0, occ_pack = 0, occ_commit = 0, occ_fused = 0, occ_single = 0;
-    uint32_t quad_mode = 0;      // page quartets: 0 = where they pay, 1 = never, 2 = wherever they are possible
-    uint64_t *d_thread_const = nullptr;
-    bool fused = true;           // restore runs verify and commit in one launch
-    unsigned long long wait_limit_ns = kWaitLimitNs;
-    uint32_t ctr_next[2] = {0, 0};  // what the device work counters will read when the next launch of
-                                    // the current call starts (the first kernel of a call zeroes them)
-    uint32_t test_drop_verify = 0;  // test hook: see gk_ctx_set_tuning
-    bool commit_reverse = true;     // commit side walks a job's pages from the last to the first
-    uint32_t l2_hints = 0;          // bit 0: verify loads evict_last, bit 1: commit loads evict_first
-    uint32_t commit_items_per_cta = 3;       // small calls: commit work items wanted per resident CTA
-    uint64_t debug_extent_cut = 0;  // bounds-checked build, tests: cache extents are reported this much smaller
-    unsigned long long *trace = nullptr;  // builds with GK_TRACE: device buffer for time stamps (tuning keys)
-    uint32_t seg_granules = 0;   // segment length in granules for the CRC modes
-    uint32_t commit_seg_tiles = 0;
-    uint32_t grid_cap = 0;       // 0: SMs * occupancy
-
-    // constant tables + sticky error word
-    uint64_t *d_init_term = nullptr;
-    uint32_t *d_error = nullptr;
-
-    // growing device workspace and pinned staging for job tables
-    uint8_t *d_ws = nullptr;
-    size_t ws_cap = 0;
-    // pinned staging for job tables, two halves used in turn: the host fills one while the
-    // upload of the previous call may still be reading the other
-    uint8_t *h_stage = nullptr;      // 2 * h_stage_cap bytes
-    size_t h_stage_cap = 0;          // bytes of one half
-    cudaEvent_t ev_stage[2] = {nullptr, nullptr};  // upload from that half has been consumed
-    uint32_t stage_next = 0;
-    cudaEvent_t ev_entry = nullptr;  // host tier: where the caller's stream stood when the call came in
-
-    // host tier
-    cudaStream_t copy_stream = nullptr;
-    uint8_t *d_slot[kSlots] = {nullptr, nullptr};
-    size_t slot_cap = 0;
-    cudaEvent_t ev_slot_free[kSlots] = {nullptr, nullptr};
-    cudaEvent_t ev_copied[kSlots] = {nullptr, nullptr};
-    bool slot_used[kSlots] = {false, false};
-    uint32_t slot_next = 0;  // the slot the next batch goes to (carried across calls)
-    bool pdl_next = false;   // the kernel just enqueued lets the next one start early (small calls)
-
-    // layer-wise restore: the codes and pages of the group in flight
-    uint8_t *d_group_tmp = nullptr;
-    size_t group_tmp_cap = 0;
-    // layer-wise calls on the device tier: the groups go in turn to this context and to a twin of it, each on a
-    // stream of its own, so that the first launches of a group overlap the last ones of the group before
-    gk_ctx *twin = nullptr;
-    bool is_twin = false;
-    cudaStream_t lw_stream[2] = {nullptr, nullptr};
-    cudaEvent_t lw_entry = nullptr;
-    cudaEvent_t lw_done[2] = {nullptr, nullptr};    // the group's work on its stream has been enqueued
-    cudaEvent_t lw_merged[2] = {nullptr, nullptr};  // the group's result arrays have been read (caller's stream)
-
-    // streaming restore: the ids 0..iota_cap-1, from which window page tables are cut
-    int32_t *d_iota = nullptr;
-    uint64_t iota_cap = 0;
-
-    // optional per-kernel timing (tuning key "profile")
-    bool profile = false;
-    struct ProfSlot { cudaEvent_t a, b; int cls; };
-    std::vector<ProfSlot> prof_pool;
-    size_t prof_used = 0;
-    double prof_ms[4] = {0, 0, 0, 0};
-    uint64_t prof_launches[4] = {0, 0, 0, 0};
-
-    // powers of x^(8 * segment bytes) for the segment lengths used recently (host arithmetic
-    // of a few microseconds per length, which small calls would otherwise pay every time)
-    struct SegPowers { uint64_t seg_bytes = 0; uint64_t x_seg = 0; std::vector<uint64_t> pw; uint64_t used = 0; };
-    SegPowers seg_cache[4];
-    uint64_t seg_cache_clock = 0;
-
-    // host tier: buffers already seen to be pinned host memory (exact start addresses)
-    std::vector<const void *> pinned_seen;
-
-    gk_stats stats{};
-    char err[512] = {0};
-};
-
 namespace {
-
-int fail(gk_ctx *c, int code, const char *fmt, ...)
-{
-    if (c) {
-        va_list ap;
-        va_start(ap, fmt);
-        vsnprintf(c->err, sizeof(c->err), fmt, ap);
-        va_end(ap);
-    }
-    return code;
-}
-
-#define GK_CUDA(c, call)                                                                      \
-    do {                                                                                      \
-        cudaError_t e_ = (call);                                                              \
-        if (e_ != cudaSuccess)                                                                \
-            return fail((c), GK_ERR_CUDA, "%s failed: %s", #call, cudaGetErrorString(e_));    \
-    } while (0)
 
 int check_geom(const gk_geom *g, GeomDev *out)
 {
@@ -239,37 +135,6 @@ int check_geom(const gk_geom *g, GeomDev *out)
     return GK_OK;
 }
 
-int check_cache(gk_ctx *c, const gk_cache *k, CacheDev *out)
-{
-    if (!k || !k->data || k->num_pages == 0) return fail(c, GK_ERR_ARG, "cache: null data or zero pages");
-    if (k->num_pages > 0x7fffffffull) return fail(c, GK_ERR_ARG, "cache: too many pages");
-    if (((uintptr_t)k->data | k->layer_stride | k->kv_stride | k->page_stride) & 15u)
-        return fail(c, GK_ERR_UNSUPPORTED, "cache: data pointer and strides must be multiples of 16 bytes");
-    if (c->gd.scale_kv) {
-        if (!k->scales) return fail(c, GK_ERR_ARG, "cache: fp8 geometry needs a scale tensor");
-        if (((uintptr_t)k->scales | k->s_layer_stride | k->s_kv_stride | k->s_page_stride) & 3u)
-            return fail(c, GK_ERR_UNSUPPORTED, "cache: scale pointer and strides must be multiples of 4 bytes");
-    }
-    out->data = (uint8_t *)k->data;
-    out->num_pages = k->num_pages;
-    out->layer_stride = k->layer_stride;
-    out->kv_stride = k->kv_stride;
-    out->page_stride = k->page_stride;
-    out->scales = (uint8_t *)k->scales;
-    out->s_layer_stride = k->s_layer_stride;
-    out->s_kv_stride = k->s_kv_stride;
-    out->s_page_stride = k->s_page_stride;
-    // where the last byte that a page table of this geometry can address lies (the bounds-checked build
-    // compares every access with these)
-    const uint64_t slab = (uint64_t)c->gd.page_tokens * c->gd.row;
-    out->data_extent = (uint64_t)(c->gd.layers - 1u) * k->layer_stride + k->kv_stride + (k->num_pages - 1u) * k->page_stride + slab;
-    out->scales_extent = c->gd.scale_kv ? (uint64_t)(c->gd.layers - 1u) * k->s_layer_stride +
-                                              (uint64_t)(c->gd.scale_kv - 1u) * k->s_kv_stride +
-                                              (k->num_pages - 1u) * k->s_page_stride + 4ull * c->gd.kv_heads
-                                        : 0u;
-    out->data_extent -= c->debug_extent_cut < out->data_extent ? c->debug_extent_cut : out->data_extent;
-    return GK_OK;
-}
 
 // Work items wanted per launch: two per resident CTA, so that small calls still fill the GPU
 // (measured: verify of 64 and of 325 GQA pages is fastest with 1-2 and 2-4 items per CTA).
@@ -952,19 +817,6 @@ int make_host_plan(gk_ctx *c, const gk_job *jobs, uint32_t n_jobs, bool allow_mi
     return GK_OK;
 }
 
-struct DeviceGuard {
-    int prev = -1;
-    explicit DeviceGuard(int dev)
-    {
-        cudaGetDevice(&prev);
-        if (prev != dev) cudaSetDevice(dev);
-        else prev = -1;
-    }
-    ~DeviceGuard()
-    {
-        if (prev >= 0) cudaSetDevice(prev);
-    }
-};
 
 }  // namespace
 
@@ -1100,6 +952,7 @@ int gk_ctx_destroy(gk_ctx *c)
     if (c->d_ws) cudaFree(c->d_ws);
     if (c->d_iota) cudaFree(c->d_iota);
     if (c->d_group_tmp) cudaFree(c->d_group_tmp);
+    if (c->d_attn) cudaFree(c->d_attn);
     if (c->d_init_term) cudaFree(c->d_init_term);
     if (c->d_thread_const) cudaFree(c->d_thread_const);
     if (c->d_error) cudaFree(c->d_error);
@@ -1206,6 +1059,7 @@ int gk_ctx_clear_error(gk_ctx *c, void *stream)
     DeviceGuard guard(c->device);
     GK_CUDA(c, cudaMemsetAsync(c->d_error, 0, 4, (cudaStream_t)stream));
     if (c->twin) GK_CUDA(c, cudaMemsetAsync(c->twin->d_error, 0, 4, (cudaStream_t)stream));
+    if (c->d_attn) GK_CUDA(c, cudaMemsetAsync(c->d_attn, 0, c->attn_counter_bytes, (cudaStream_t)stream));
     return GK_OK;
 }
 
@@ -1217,7 +1071,7 @@ int gk_pack_batch(gk_ctx *c, const gk_cache *src, const gk_job *jobs, uint32_t n
     if (!jobs) return fail(c, GK_ERR_ARG, "null job array");
     DeviceGuard guard(c->device);
     cudaStream_t st = (cudaStream_t)stream;
-    CacheDev cd;
+    CacheDev cd{};
     int rc = check_cache(c, src, &cd);
     if (rc != GK_OK) return rc;
     for (uint32_t j = 0; j < n_jobs; ++j)
@@ -1352,7 +1206,7 @@ int gk_restore(gk_ctx *c, const gk_job *jobs, uint32_t n_jobs, const gk_cache *d
     if (!jobs || !mask_dev || !first_bad_page_dev) return fail(c, GK_ERR_ARG, "null jobs, mask or first_bad_page");
     DeviceGuard guard(c->device);
     cudaStream_t st = (cudaStream_t)stream;
-    CacheDev cd;
+    CacheDev cd{};
     int rc = check_cache(c, dst, &cd);
     if (rc != GK_OK) return rc;
 
@@ -1425,7 +1279,7 @@ int gk_verify(gk_ctx *c, const gk_job *jobs, uint32_t n_jobs, const gk_cache *ds
     if (!jobs || !mask_dev || !first_bad_page_dev) return fail(c, GK_ERR_ARG, "null jobs, mask or first_bad_page");
     DeviceGuard guard(c->device);
     cudaStream_t st = (cudaStream_t)stream;
-    CacheDev cd;
+    CacheDev cd{};
     Tiling tlv, tlc;
     WorkDev w;
     uint64_t pages, bytes;
@@ -1457,7 +1311,7 @@ int gk_commit(gk_ctx *c, const gk_job *jobs, uint32_t n_jobs, const gk_cache *ds
     if (!jobs || !mask_dev) return fail(c, GK_ERR_ARG, "null jobs or mask");
     DeviceGuard guard(c->device);
     cudaStream_t st = (cudaStream_t)stream;
-    CacheDev cd;
+    CacheDev cd{};
     Tiling tlv, tlc;
     WorkDev w;
     uint64_t pages, bytes;
@@ -1488,7 +1342,7 @@ static int restore_host_impl(gk_ctx *c, const gk_job *jobs, uint32_t n_jobs, con
     if (!jobs || !mask_dev || !first_bad_page_dev) return fail(c, GK_ERR_ARG, "null jobs, mask or first_bad_page");
     DeviceGuard guard(c->device);
     cudaStream_t st = (cudaStream_t)stream;
-    CacheDev cd;
+    CacheDev cd{};
     int rc = check_cache(c, dst, &cd);
     if (rc != GK_OK) return rc;
     if (order_after_stream) {
@@ -1566,7 +1420,7 @@ int gk_restore_stream(gk_ctx *c, const gk_job *jobs, uint32_t n_jobs, const gk_c
     if (!jobs || !mask_dev || !first_bad_page_dev) return fail(c, GK_ERR_ARG, "null jobs, mask or first_bad_page");
     DeviceGuard guard(c->device);
     cudaStream_t st = (cudaStream_t)stream;
-    CacheDev cd;
+    CacheDev cd{};
     int rc = check_cache(c, ring, &cd);
     if (rc != GK_OK) return rc;
     std::vector<uint32_t> np(n_jobs);
@@ -1611,7 +1465,7 @@ int gk_pack_host(gk_ctx *c, const gk_cache *src, const gk_job *jobs, uint32_t n_
     if (!jobs) return fail(c, GK_ERR_ARG, "null job array");
     DeviceGuard guard(c->device);
     cudaStream_t st = (cudaStream_t)stream;
-    CacheDev cd;
+    CacheDev cd{};
     int rc = check_cache(c, src, &cd);
     if (rc != GK_OK) return rc;
     HostPlan hp;

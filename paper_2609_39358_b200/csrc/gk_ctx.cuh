@@ -1,0 +1,171 @@
+// gk_ctx.cuh -- the context behind a gk_ctx handle and the small host helpers (errors, cache checks, the
+// current device) that every file with entry points shares.  Not part of the public interface.
+#pragma once
+
+#include <cstdarg>
+#include <cstdio>
+#include <vector>
+
+#include "../../include/gk.h"
+#include "gk_device.cuh"
+
+namespace gk {
+constexpr int kSlots = 2;  // host-tier staging ring
+
+}  // namespace gk
+
+struct gk_ctx {
+    gk_geom geom{};
+    gk::GeomDev gd{};
+    int device = 0;
+    int sm_count = 0;
+    int occ_verify = 0, occ_pack = 0, occ_commit = 0, occ_fused = 0, occ_single = 0;
+    uint32_t quad_mode = 0;      // page quartets: 0 = where they pay, 1 = never, 2 = wherever they are possible
+    uint64_t *d_thread_const = nullptr;
+    bool fused = true;           // restore runs verify and commit in one launch
+    unsigned long long wait_limit_ns = gk::kWaitLimitNs;
+    uint32_t ctr_next[2] = {0, 0};  // what the device work counters will read when the next launch of
+                                    // the current call starts (the first kernel of a call zeroes them)
+    uint32_t test_drop_verify = 0;  // test hook: see gk_ctx_set_tuning
+    bool commit_reverse = true;     // commit side walks a job's pages from the last to the first
+    uint32_t l2_hints = 0;          // bit 0: verify loads evict_last, bit 1: commit loads evict_first
+    uint32_t commit_items_per_cta = 3;       // small calls: commit work items wanted per resident CTA
+    uint64_t debug_extent_cut = 0;  // bounds-checked build, tests: cache extents are reported this much smaller
+    unsigned long long *trace = nullptr;  // builds with GK_TRACE: device buffer for time stamps (tuning keys)
+    uint32_t seg_granules = 0;   // segment length in granules for the CRC modes
+    uint32_t commit_seg_tiles = 0;
+    uint32_t grid_cap = 0;       // 0: SMs * occupancy
+
+    // constant tables + sticky error word
+    uint64_t *d_init_term = nullptr;
+    uint32_t *d_error = nullptr;
+
+    // growing device workspace and pinned staging for job tables
+    uint8_t *d_ws = nullptr;
+    size_t ws_cap = 0;
+    // pinned staging for job tables, two halves used in turn: the host fills one while the
+    // upload of the previous call may still be reading the other
+    uint8_t *h_stage = nullptr;      // 2 * h_stage_cap bytes
+    size_t h_stage_cap = 0;          // bytes of one half
+    cudaEvent_t ev_stage[2] = {nullptr, nullptr};  // upload from that half has been consumed
+    uint32_t stage_next = 0;
+    cudaEvent_t ev_entry = nullptr;  // host tier: where the caller's stream stood when the call came in
+
+    // host tier
+    cudaStream_t copy_stream = nullptr;
+    uint8_t *d_slot[gk::kSlots] = {nullptr, nullptr};
+    size_t slot_cap = 0;
+    cudaEvent_t ev_slot_free[gk::kSlots] = {nullptr, nullptr};
+    cudaEvent_t ev_copied[gk::kSlots] = {nullptr, nullptr};
+    bool slot_used[gk::kSlots] = {false, false};
+    uint32_t slot_next = 0;  // the slot the next batch goes to (carried across calls)
+    bool pdl_next = false;   // the kernel just enqueued lets the next one start early (small calls)
+
+    // layer-wise restore: the codes and pages of the group in flight
+    uint8_t *d_group_tmp = nullptr;
+    size_t group_tmp_cap = 0;
+    // layer-wise calls on the device tier: the groups go in turn to this context and to a twin of it, each on a
+    // stream of its own, so that the first launches of a group overlap the last ones of the group before
+    gk_ctx *twin = nullptr;
+    bool is_twin = false;
+    cudaStream_t lw_stream[2] = {nullptr, nullptr};
+    cudaEvent_t lw_entry = nullptr;
+    cudaEvent_t lw_done[2] = {nullptr, nullptr};    // the group's work on its stream has been enqueued
+    cudaEvent_t lw_merged[2] = {nullptr, nullptr};  // the group's result arrays have been read (caller's stream)
+
+    // streaming restore: the ids 0..iota_cap-1, from which window page tables are cut
+    int32_t *d_iota = nullptr;
+    uint64_t iota_cap = 0;
+
+    // gk_attention: one block of a fixed size per context (join counters, then partial results)
+    uint8_t *d_attn = nullptr;
+    size_t attn_counter_bytes = 0;
+
+    // optional per-kernel timing (tuning key "profile")
+    bool profile = false;
+    struct ProfSlot { cudaEvent_t a, b; int cls; };
+    std::vector<ProfSlot> prof_pool;
+    size_t prof_used = 0;
+    double prof_ms[4] = {0, 0, 0, 0};
+    uint64_t prof_launches[4] = {0, 0, 0, 0};
+
+    // powers of x^(8 * segment bytes) for the segment lengths used recently (host arithmetic
+    // of a few microseconds per length, which small calls would otherwise pay every time)
+    struct SegPowers { uint64_t seg_bytes = 0; uint64_t x_seg = 0; std::vector<uint64_t> pw; uint64_t used = 0; };
+    SegPowers seg_cache[4];
+    uint64_t seg_cache_clock = 0;
+
+    // host tier: buffers already seen to be pinned host memory (exact start addresses)
+    std::vector<const void *> pinned_seen;
+
+    gk_stats stats{};
+    char err[512] = {0};
+};
+
+namespace gk {
+
+inline int fail(gk_ctx *c, int code, const char *fmt, ...)
+{
+    if (c) {
+        va_list ap;
+        va_start(ap, fmt);
+        vsnprintf(c->err, sizeof(c->err), fmt, ap);
+        va_end(ap);
+    }
+    return code;
+}
+
+#define GK_CUDA(c, call)                                                                      \
+    do {                                                                                      \
+        cudaError_t e_ = (call);                                                              \
+        if (e_ != cudaSuccess)                                                                \
+            return fail((c), GK_ERR_CUDA, "%s failed: %s", #call, cudaGetErrorString(e_));    \
+    } while (0)
+
+inline int check_cache(gk_ctx *c, const gk_cache *k, CacheDev *out)
+{
+    if (!k || !k->data || k->num_pages == 0) return fail(c, GK_ERR_ARG, "cache: null data or zero pages");
+    if (k->num_pages > 0x7fffffffull) return fail(c, GK_ERR_ARG, "cache: too many pages");
+    if (((uintptr_t)k->data | k->layer_stride | k->kv_stride | k->page_stride) & 15u)
+        return fail(c, GK_ERR_UNSUPPORTED, "cache: data pointer and strides must be multiples of 16 bytes");
+    if (c->gd.scale_kv) {
+        if (!k->scales) return fail(c, GK_ERR_ARG, "cache: fp8 geometry needs a scale tensor");
+        if (((uintptr_t)k->scales | k->s_layer_stride | k->s_kv_stride | k->s_page_stride) & 3u)
+            return fail(c, GK_ERR_UNSUPPORTED, "cache: scale pointer and strides must be multiples of 4 bytes");
+    }
+    out->data = (uint8_t *)k->data;
+    out->num_pages = k->num_pages;
+    out->layer_stride = k->layer_stride;
+    out->kv_stride = k->kv_stride;
+    out->page_stride = k->page_stride;
+    out->scales = (uint8_t *)k->scales;
+    out->s_layer_stride = k->s_layer_stride;
+    out->s_kv_stride = k->s_kv_stride;
+    out->s_page_stride = k->s_page_stride;
+    // where the last byte that a page table of this geometry can address lies (the bounds-checked build
+    // compares every access with these)
+    const uint64_t slab = (uint64_t)c->gd.page_tokens * c->gd.row;
+    out->data_extent = (uint64_t)(c->gd.layers - 1u) * k->layer_stride + k->kv_stride + (k->num_pages - 1u) * k->page_stride + slab;
+    out->scales_extent = c->gd.scale_kv ? (uint64_t)(c->gd.layers - 1u) * k->s_layer_stride +
+                                              (uint64_t)(c->gd.scale_kv - 1u) * k->s_kv_stride +
+                                              (k->num_pages - 1u) * k->s_page_stride + 4ull * c->gd.kv_heads
+                                        : 0u;
+    out->data_extent -= c->debug_extent_cut < out->data_extent ? c->debug_extent_cut : out->data_extent;
+    return GK_OK;
+}
+
+struct DeviceGuard {
+    int prev = -1;
+    explicit DeviceGuard(int dev)
+    {
+        cudaGetDevice(&prev);
+        if (prev != dev) cudaSetDevice(dev);
+        else prev = -1;
+    }
+    ~DeviceGuard()
+    {
+        if (prev >= 0) cudaSetDevice(prev);
+    }
+};
+
+}  // namespace gk

@@ -1,0 +1,239 @@
+// gk_ops.cu -- host side of the calls that use the cache: gk_append and gk_attention (include/gk.h).
+// Argument checks, launch shapes and the attention workspace; the work is in the kernels.
+#include "gk_ctx.cuh"
+
+#include <cmath>
+
+#include "gk_append.cuh"
+#include "gk_attend.cuh"
+
+using namespace gk;
+
+namespace {
+
+int check_batch(gk_ctx *c, const gk_batch *b, SeqsDev *out)
+{
+    if (!b) return fail(c, GK_ERR_ARG, "batch: null");
+    if (b->n_seqs > 0x7ffffffeu || b->n_tokens > 0x7fffffffu || b->max_pages > 0x7fffffffu)
+        return fail(c, GK_ERR_ARG, "batch: too many sequences, tokens or pages");
+    if (b->n_seqs == 0 && b->n_tokens != 0) return fail(c, GK_ERR_ARG, "batch: tokens without sequences");
+    if (b->n_tokens == 0) return GK_OK;
+    if (!b->page_table || !b->kv_len || b->max_pages == 0) return fail(c, GK_ERR_ARG, "batch: null page table or lengths");
+    if (b->n_seqs > 1 && b->table_stride < b->max_pages) return fail(c, GK_ERR_ARG, "batch: table rows overlap");
+    if (!b->q_start && b->n_tokens != b->n_seqs)
+        return fail(c, GK_ERR_ARG, "batch: without q_start every sequence has one token");
+    if (((uintptr_t)b->page_table | (uintptr_t)b->q_start | (uintptr_t)b->kv_len) & 3u)
+        return fail(c, GK_ERR_UNSUPPORTED, "batch: arrays must be 4-byte aligned");
+    *out = SeqsDev{b->page_table, b->table_stride, b->q_start, b->kv_len, b->status, b->n_seqs, b->n_tokens, b->max_pages};
+    return GK_OK;
+}
+
+int check_layer(gk_ctx *c, const gk_cache *k, uint32_t layer, LayerDev *out)
+{
+    CacheDev cd{};
+    const int rc = check_cache(c, k, &cd);
+    if (rc != GK_OK) return rc;
+    if (layer >= c->geom.layers) return fail(c, GK_ERR_ARG, "layer %u of %u", layer, c->geom.layers);
+    const gk_geom &g = c->geom;
+    if (g.head_dim % 16 != 0 || g.head_dim > 256)
+        return fail(c, GK_ERR_UNSUPPORTED, "head_dim %u: a multiple of 16 up to 256 is supported", g.head_dim);
+    out->k = cd.data + layer * cd.layer_stride;
+    out->v = out->k + cd.kv_stride;
+    out->page = cd.page_stride;
+    out->tok = c->gd.head_major ? c->gd.hrow : c->gd.row;
+    out->head = c->gd.head_major ? c->gd.hrow * g.page_tokens : c->gd.hrow;
+    out->ks = out->vs = nullptr;
+    out->s_page = 0;
+    if (g.scale_kv) {
+        out->ks = (float *)(cd.scales + layer * cd.s_layer_stride);
+        out->vs = (float *)(cd.scales + layer * cd.s_layer_stride + (g.scale_kv == 2 ? cd.s_kv_stride : 0));
+        out->s_page = cd.s_page_stride / 4;
+    }
+    out->num_pages = (uint32_t)cd.num_pages;
+    out->H = g.kv_heads;
+    out->D = g.head_dim;
+    out->T = g.page_tokens;
+    out->by_T = FastDiv::make(g.page_tokens);
+    return GK_OK;
+}
+
+int check_rows(gk_ctx *c, const gk_rows *r, const char *name)
+{
+    if (!r || !r->data) return fail(c, GK_ERR_ARG, "%s: null", name);
+    if (((uintptr_t)r->data & 15u) || (r->token_stride & 7u) || (r->head_stride & 7u))
+        return fail(c, GK_ERR_UNSUPPORTED, "%s: 16-byte aligned data and strides that are multiples of 8 elements are needed", name);
+    return GK_OK;
+}
+
+RowsDev rows_dev(const gk_rows *r)
+{
+    return RowsDev{(const __nv_bfloat16 *)r->data, r->token_stride, r->head_stride};
+}
+
+int check_rope(gk_ctx *c, const gk_rope *r, RopeDev *out)
+{
+    *out = RopeDev{};
+    if (!r || r->rotary_dim == 0) return GK_OK;
+    if (!r->cos_sin || r->max_pos == 0) return fail(c, GK_ERR_ARG, "rope: null table");
+    if (r->reserved != 0 || r->interleaved > 1 || r->axes < 1 || r->axes > 3) return fail(c, GK_ERR_ARG, "rope: bad field");
+    if (r->rotary_dim > c->geom.head_dim) return fail(c, GK_ERR_ARG, "rope: rotary_dim above head_dim");
+    if (r->rotary_dim % 16 != 0) return fail(c, GK_ERR_UNSUPPORTED, "rope: rotary_dim must be a multiple of 16");
+    if (r->max_pos > 0x7fffffffu) return fail(c, GK_ERR_ARG, "rope: too many positions");
+    if ((uintptr_t)r->cos_sin & 15u) return fail(c, GK_ERR_UNSUPPORTED, "rope: the table must be 16-byte aligned");
+    if (r->axes > 1 && !r->positions) return fail(c, GK_ERR_ARG, "rope: several axes need positions");
+    if ((uintptr_t)r->positions & 3u) return fail(c, GK_ERR_UNSUPPORTED, "rope: positions must be 4-byte aligned");
+    uint64_t sum = 0;
+    for (uint32_t a = 0; a < r->axes; ++a) sum += r->section[a];
+    if (sum != r->rotary_dim / 2) return fail(c, GK_ERR_ARG, "rope: the sections must sum to rotary_dim / 2");
+    out->cos_sin = r->cos_sin;
+    out->positions = r->positions;
+    out->max_pos = r->max_pos;
+    out->R = r->rotary_dim;
+    out->interleaved = r->interleaved;
+    out->axes = r->axes;
+    out->end0 = r->section[0];
+    out->end1 = r->axes > 1 ? r->section[0] + r->section[1] : r->section[0];
+    if (r->axes == 1) out->end0 = out->end1 = r->rotary_dim / 2;
+    return GK_OK;
+}
+
+// Workspace of gk_attention: join counters, then two partial results per CTA of the largest grid.
+constexpr size_t kAttnCounterBytes = 4096;
+constexpr int kAttnMaxCtas = 1024;
+
+int ensure_attention(gk_ctx *c)
+{
+    if (c->d_attn) return GK_OK;
+    const size_t part = (size_t)(kAttendRows * 256 + 2 * kAttendRows) * 4;
+    const size_t bytes = kAttnCounterBytes + 2 * (size_t)kAttnMaxCtas * part;
+    if (cudaMalloc(&c->d_attn, bytes) != cudaSuccess) {
+        cudaGetLastError();
+        c->d_attn = nullptr;
+        return fail(c, GK_ERR_NOMEM, "attention workspace of %zu bytes", bytes);
+    }
+    c->attn_counter_bytes = kAttnCounterBytes;
+    if (cudaMemset(c->d_attn, 0, kAttnCounterBytes) != cudaSuccess) {
+        cudaGetLastError();
+        cudaFree(c->d_attn);
+        c->d_attn = nullptr;
+        return fail(c, GK_ERR_CUDA, "attention workspace");
+    }
+    c->stats.allocations++;
+    return GK_OK;
+}
+
+template <bool FP8, int DP>
+int launch_attend(gk_ctx *c, const AttendParams &P, cudaStream_t st)
+{
+    using C = AttendCfg<FP8, DP>;
+    static int occ = 0;  // the same on every sm_100 device
+    if (occ == 0) {
+        int n = 0;
+        GK_CUDA(c, cudaFuncSetAttribute(attend_kernel<FP8, DP>, cudaFuncAttributeMaxDynamicSharedMemorySize, C::SMEM));
+        GK_CUDA(c, cudaOccupancyMaxActiveBlocksPerMultiprocessor(&n, attend_kernel<FP8, DP>, kAttendThreads, C::SMEM));
+        occ = n > 0 ? n : 1;
+    }
+    int grid = c->sm_count * occ;
+    if (grid > kAttnMaxCtas) grid = kAttnMaxCtas;
+    attend_kernel<FP8, DP><<<grid, kAttendThreads, C::SMEM, st>>>(P);
+    GK_CUDA(c, cudaGetLastError());
+    c->stats.kernels_launched++;
+    return GK_OK;
+}
+
+}  // namespace
+
+extern "C" {
+
+int gk_append(gk_ctx *c, const gk_cache *dst, uint32_t layer, const gk_batch *batch, const gk_rope *rope,
+              const gk_rows *k, const gk_rows *v, uint32_t q_heads, const gk_rows *q, const gk_rows *q_out, void *stream)
+{
+    if (!c) return GK_ERR_ARG;
+    AppendParams P{};
+    int rc;
+    if ((rc = check_batch(c, batch, &P.seqs)) != GK_OK) return rc;
+    if ((rc = check_layer(c, dst, layer, &P.cache)) != GK_OK) return rc;
+    if ((rc = check_rope(c, rope, &P.rope)) != GK_OK) return rc;
+    if (batch->n_tokens == 0) return GK_OK;
+    if ((rc = check_rows(c, k, "k")) != GK_OK || (rc = check_rows(c, v, "v")) != GK_OK) return rc;
+    P.k = rows_dev(k);
+    P.v = rows_dev(v);
+    if (q) {
+        if (q_heads == 0) return fail(c, GK_ERR_ARG, "q without heads");
+        if ((rc = check_rows(c, q, "q")) != GK_OK || (rc = check_rows(c, q_out, "q_out")) != GK_OK) return rc;
+        P.q = rows_dev(q);
+        P.q_out = (__nv_bfloat16 *)q_out->data;
+        P.qo_tok = q_out->token_stride;
+        P.qo_head = q_out->head_stride;
+        P.Hq = q_heads;
+    }
+    DeviceGuard guard(c->device);
+    const bool fp8 = c->geom.dtype == GK_FP8_E4M3;
+    P.chunks = c->geom.head_dim / 16;
+    P.by_chunks = FastDiv::make(P.chunks);
+    const uint64_t per_token = ((uint64_t)P.Hq + (fp8 ? 0u : 2u * c->geom.kv_heads)) * P.chunks;
+    const uint64_t items = per_token * batch->n_tokens;
+    if (per_token > 0x7fffffffull || items > 0x7fffff00ull) return fail(c, GK_ERR_TOO_LARGE, "append: too many tokens times heads");
+    P.by_row = FastDiv::make(per_token ? (uint32_t)per_token : 1u);
+    uint64_t grid = (items + kAppendThreads - 1) / kAppendThreads;
+    if (fp8) {
+        P.shared_scale = c->geom.scale_kv == 1;
+        P.head_groups = (c->geom.kv_heads + kAppendWarps - 1) / kAppendWarps;
+        // a sequence of n rows touches at most n / T + 2 pages
+        const uint64_t slots = batch->q_start ? batch->n_tokens / c->geom.page_tokens + 2ull * batch->n_seqs : batch->n_seqs;
+        if (slots * P.head_groups + grid > 0x7fffffffull) return fail(c, GK_ERR_TOO_LARGE, "append: too many pages times heads");
+        P.unit_slots = (uint32_t)slots;
+        P.unit_ctas = (uint32_t)(slots * P.head_groups);
+        grid += P.unit_ctas;
+        append_kernel<true><<<(unsigned)grid, kAppendThreads, 0, (cudaStream_t)stream>>>(P);
+    } else {
+        append_kernel<false><<<(unsigned)grid, kAppendThreads, 0, (cudaStream_t)stream>>>(P);
+    }
+    GK_CUDA(c, cudaGetLastError());
+    c->stats.kernels_launched++;
+    return GK_OK;
+}
+
+int gk_attention(gk_ctx *c, const gk_cache *cache, uint32_t layer, const gk_batch *batch, uint32_t q_heads,
+                 const gk_rows *q, const gk_rows *out, float *lse, float scale, uint32_t window, uint32_t flags, void *stream)
+{
+    if (!c) return GK_ERR_ARG;
+    AttendParams P{};
+    int rc;
+    if ((rc = check_batch(c, batch, &P.seqs)) != GK_OK) return rc;
+    if ((rc = check_layer(c, cache, layer, &P.cache)) != GK_OK) return rc;
+    if (flags & ~GK_ATTN_FULL) return fail(c, GK_ERR_ARG, "attention: unknown flag");
+    if (q_heads == 0 || q_heads % c->geom.kv_heads != 0)
+        return fail(c, GK_ERR_ARG, "attention: %u query heads over %u key heads", q_heads, c->geom.kv_heads);
+    if (!std::isfinite(scale)) return fail(c, GK_ERR_ARG, "attention: the scale is not finite");
+    DeviceGuard guard(c->device);
+    if ((rc = ensure_attention(c)) != GK_OK) return rc;
+    if (batch->n_tokens == 0) return GK_OK;
+    if ((rc = check_rows(c, q, "q")) != GK_OK || (rc = check_rows(c, out, "out")) != GK_OK) return rc;
+    if ((uintptr_t)lse & 3u) return fail(c, GK_ERR_UNSUPPORTED, "attention: lse must be 4-byte aligned");
+    if ((uint64_t)batch->n_tokens * q_heads > 0x7fffff00ull) return fail(c, GK_ERR_TOO_LARGE, "attention: too many tokens times heads");
+    P.q = (const __nv_bfloat16 *)q->data;
+    P.q_tok = q->token_stride;
+    P.q_head = q->head_stride;
+    P.out = (__nv_bfloat16 *)out->data;
+    P.o_tok = out->token_stride;
+    P.o_head = out->head_stride;
+    P.lse = lse;
+    P.Hq = q_heads;
+    P.G = q_heads / c->geom.kv_heads;
+    P.by_G = FastDiv::make(P.G);
+    P.scale_log2 = (float)((double)scale * 1.4426950408889634);
+    P.causal = (flags & GK_ATTN_FULL) ? 0u : 1u;
+    P.window = window;
+    P.counters = (uint32_t *)c->d_attn;
+    P.parts = (float *)(c->d_attn + kAttnCounterBytes);
+    const cudaStream_t st = (cudaStream_t)stream;
+    const uint32_t D = c->geom.head_dim;
+    if (c->geom.dtype == GK_FP8_E4M3)
+        return D <= 64 ? launch_attend<true, 64>(c, P, st) : D <= 128 ? launch_attend<true, 128>(c, P, st)
+                                                                    : launch_attend<true, 256>(c, P, st);
+    return D <= 64 ? launch_attend<false, 64>(c, P, st) : D <= 128 ? launch_attend<false, 128>(c, P, st)
+                                                                  : launch_attend<false, 256>(c, P, st);
+}
+
+}  // extern "C"

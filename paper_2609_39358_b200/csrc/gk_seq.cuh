@@ -1,0 +1,85 @@
+// gk_seq.cuh -- what the kernels that append to the cache and attend over it share: the device view of
+// a batch of sequences and of one layer of the paged cache.  Not part of the public interface.
+#pragma once
+
+#include <cstdint>
+#include <cuda_bf16.h>
+#include <cuda_fp16.h>
+#include <cuda_fp8.h>
+#include <cuda_runtime.h>
+
+namespace gk {
+
+// n / d for 0 <= n < 2^31 by one multiplication (round-up method: m = ceil(2^(31+l) / d), l = ceil(log2 d))
+struct FastDiv {
+    uint32_t d, m, s;
+    __host__ static FastDiv make(uint32_t d)
+    {
+        FastDiv f{d, 0, 0};
+        while ((1ull << f.s) < d) ++f.s;
+        f.m = (uint32_t)(((1ull << (31 + f.s)) + d - 1) / d);
+        return f;
+    }
+    __device__ __forceinline__ uint32_t div(uint32_t n) const
+    {
+        return d == 1u ? n : (uint32_t)(((uint64_t)n * m) >> (31 + s));
+    }
+};
+
+struct SeqsDev {
+    const int32_t *page_table;
+    uint64_t table_stride;
+    const int32_t *q_start;  // null: one token per sequence
+    const int32_t *kv_len;
+    uint8_t *status;
+    uint32_t n_seqs, n_tokens, max_pages;
+};
+
+// One layer of the cache.  A value of token row r of page g, head h, dimension d lies at
+// k (or v) + g*page + r*tok + h*head + d*elem.
+struct LayerDev {
+    uint8_t *k, *v;
+    uint64_t page;       // bytes
+    uint32_t tok, head;  // bytes
+    float *ks, *vs;      // fp8: scale of (page g, head h) at ks + g*s_page + h (the same array if K and V share it)
+    uint64_t s_page;     // floats
+    uint32_t num_pages;
+    uint32_t H, D, T;
+    FastDiv by_T;
+};
+
+struct SeqSpan {
+    int q0, q_len, kv;
+};
+
+// Rows and tokens of sequence s.  Row offsets are clamped to the token tensors, so that a bad offset
+// array can never lead outside them.
+__device__ __forceinline__ SeqSpan seq_span(const SeqsDev &b, uint32_t s)
+{
+    SeqSpan r;
+    if (b.q_start) {
+        const int n = (int)b.n_tokens;
+        r.q0 = min(max(__ldg(b.q_start + s), 0), n);
+        r.q_len = max(min(max(__ldg(b.q_start + s + 1), 0), n) - r.q0, 0);
+    } else {
+        r.q0 = (int)s;
+        r.q_len = 1;
+    }
+    r.kv = max(__ldg(b.kv_len + s), 0);
+    return r;
+}
+
+// The sequence that row i belongs to: the last one that starts at or before it.
+__device__ __forceinline__ uint32_t seq_of_row(const SeqsDev &b, uint32_t i)
+{
+    if (!b.q_start) return i;
+    uint32_t lo = 0, hi = b.n_seqs;
+    while (hi - lo > 1u) {
+        const uint32_t mid = (lo + hi) >> 1;
+        if (__ldg(b.q_start + mid) <= (int)i) lo = mid;
+        else hi = mid;
+    }
+    return lo;
+}
+
+}  // namespace gk
