@@ -14,7 +14,7 @@ DEBUG_LIB_PATH = os.path.join(_HERE, "libgk_debug.so")   # the bounds-checked bu
 # Every file by itself, then one link.  --use_fast_math is for the integer kernels of gk_api.cu only: the operators on
 # the cache state each approximation where they make it.
 _SOURCES = {"gk_api.cu": ["--use_fast_math"], "gk_ops.cu": []}
-_DEPS = ["gk_api.cu", "gk_ops.cu", "gk_ctx.cuh", "gk_seq.cuh", "gk_append.cuh", "gk_attend.cuh", "gk_kernels.cuh", "gk_device.cuh", "gk_sha256.cuh", "gk_gf2_generated.inc", "gen_tables.py",
+_DEPS = ["gk_api.cu", "gk_ops.cu", "gk_ctx.cuh", "gk_seq.cuh", "gk_append.cuh", "gk_attend.cuh", "gk_attend_rows.cuh", "gk_kernels.cuh", "gk_device.cuh", "gk_sha256.cuh", "gk_gf2_generated.inc", "gen_tables.py",
          os.path.join("..", "..", "include", "gk.h")]
 
 

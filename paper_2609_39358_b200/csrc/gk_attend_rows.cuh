@@ -1,0 +1,939 @@
+// gk_attend_rows.cuh -- attention of many rows over the paged cache (gk_attention): prompts, chunks and
+// questions, bound by the tensor cores.
+//
+// The mathematics is attend_kernel's (gk_attend.cuh); the two products run on tcgen05.mma.  A CTA works on a
+// block of 256 query rows of one key head -- two tiles of 128, so that one tile's softmax runs while the
+// tensor cores work on the other -- and walks the sequence in tiles of 128 tokens:
+//
+//   S = Q K^T       Q and K in shared memory (128-byte swizzle), S fp32 in tensor memory
+//   P = exp2(S - m) one thread per row: row sums and maxima need no exchange.  P replaces S in tensor memory.
+//   O += P V        P from tensor memory, V in shared memory, O fp32 in tensor memory
+//
+// O is multiplied by exp2(m_old - m_new) only when some row's maximum rose by more than kRise since it was
+// last fixed (the weights then reach 2^kRise, which neither P's type nor the fp32 sums mind); after the first
+// tiles of a row that is rare.
+//
+// Warps: 0-3 and 4-7 softmax and output of the two tiles, 8-11 load K and V through the page table (bf16:
+// 16-byte asynchronous copies; fp8: loads, conversion to f16, shared-memory stores), 12 issues the MMAs.
+//
+// Work is dealt out as in attend_kernel: the token tiles of all blocks lie in one line, every CTA takes an equal
+// stretch, parts of a block meet in the workspace.
+#pragma once
+
+#include "gk_attend.cuh"
+#include "gk_device.cuh"
+
+namespace gk {
+
+constexpr int kRowsTile = 128;               // query rows of a tile, tokens of a tile
+constexpr int kRowsBlock = 2 * kRowsTile;
+constexpr int kRowsThreads = 512;
+constexpr int kRowsStages = 4;               // K and V tiles in shared memory, taken in turn: K, V, K, V
+constexpr int kRowsScaleSlots = 4;
+
+struct RowsParams {
+    AttendParams a;
+    float scale_log2;     // |scale| * log2(e); the sign goes into the queries
+    float q_sign;         // 1, -1, or 0 with a scale of 0
+    uint32_t *error;
+    unsigned long long wait_limit_ns;
+};
+
+template <bool FP8, int DP>
+struct RowsCfg {
+    static constexpr int HALVES = DP / 64;                    // 64 values of 16 bits = one swizzled row of 128 bytes
+    static constexpr int TILE_BYTES = kRowsTile * DP * 2;
+    static constexpr int Q_OFF = 0;
+    static constexpr int KV_OFF = 2 * TILE_BYTES;
+    static constexpr int END = KV_OFF + kRowsStages * TILE_BYTES;
+    static constexpr int SMEM = END + 1024;                   // room to align the tiles
+    static constexpr int PART_FLOATS = kRowsBlock * (DP + 2);
+    static constexpr float kRise = FP8 ? 4.f : 8.f;
+    static constexpr float kUp = FP8 ? 2048.f : 1.f;          // f16 weights: up to 2^4 * 2^11
+};
+
+// ---- tcgen05 ----
+
+__device__ __forceinline__ void tc_fence_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
+__device__ __forceinline__ void tc_fence_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
+__device__ __forceinline__ void tc_wait_ld() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
+__device__ __forceinline__ void tc_wait_st() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
+__device__ __forceinline__ void fence_async_smem() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
+
+__device__ __forceinline__ void tc_commit(uint32_t bar)
+{
+    asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(bar) : "memory");
+}
+
+// shared-memory operand descriptor: 128-byte swizzle, groups of 8 rows 1024 bytes apart; `lead` is the distance
+// between 64-value pieces of an operand whose contiguous dimension is not the summed one (V)
+__device__ __forceinline__ uint64_t tc_desc(uint32_t addr, uint32_t lead)
+{
+    return (uint64_t)((addr & 0x3ffffu) >> 4) | ((uint64_t)(lead >> 4) << 16) | ((uint64_t)(1024u >> 4) << 32) |
+           (1ull << 46) | (2ull << 61);
+}
+
+// M = 128, fp32 accumulators; f16 or bf16 operands; b_mn: B's contiguous dimension is N
+__host__ __device__ constexpr uint32_t tc_idesc(bool f16, int n, bool b_mn)
+{
+    return (1u << 4) | ((f16 ? 0u : 1u) << 7) | ((f16 ? 0u : 1u) << 10) | ((b_mn ? 1u : 0u) << 16) | ((uint32_t)(n >> 3) << 17) |
+           ((128u >> 4) << 24);
+}
+
+__device__ __forceinline__ void tc_mma_ss(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, bool add)
+{
+    asm volatile("{ .reg .pred p; setp.ne.u32 p, %4, 0; tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p; }" ::"r"(d),
+                 "l"(a), "l"(b), "r"(idesc), "r"((uint32_t)add)
+                 : "memory");
+}
+__device__ __forceinline__ void tc_mma_ts(uint32_t d, uint32_t a, uint64_t b, uint32_t idesc, bool add)
+{
+    asm volatile("{ .reg .pred p; setp.ne.u32 p, %4, 0; tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p; }" ::"r"(d),
+                 "r"(a), "l"(b), "r"(idesc), "r"((uint32_t)add)
+                 : "memory");
+}
+
+#define GK_R8(r, o) "=r"(r[o]), "=r"(r[o + 1]), "=r"(r[o + 2]), "=r"(r[o + 3]), "=r"(r[o + 4]), "=r"(r[o + 5]), "=r"(r[o + 6]), "=r"(r[o + 7])
+#define GK_W8(r, o) "r"(r[o]), "r"(r[o + 1]), "r"(r[o + 2]), "r"(r[o + 3]), "r"(r[o + 4]), "r"(r[o + 5]), "r"(r[o + 6]), "r"(r[o + 7])
+
+// 32 consecutive columns of this thread's row
+__device__ __forceinline__ void tc_ld32(uint32_t *r, uint32_t addr)
+{
+    asm volatile("tcgen05.ld.sync.aligned.32x32b.x32.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,"
+                 "%16,%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31}, [%32];"
+                 : GK_R8(r, 0), GK_R8(r, 8), GK_R8(r, 16), GK_R8(r, 24)
+                 : "r"(addr));
+}
+__device__ __forceinline__ void tc_st32(uint32_t addr, const uint32_t *r)
+{
+    asm volatile("tcgen05.st.sync.aligned.32x32b.x32.b32 [%32], {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,"
+                 "%16,%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31};" ::GK_W8(r, 0), GK_W8(r, 8), GK_W8(r, 16),
+                 GK_W8(r, 24), "r"(addr)
+                 : "memory");
+}
+__device__ __forceinline__ void tc_st16(uint32_t addr, const uint32_t *r)
+{
+    asm volatile("tcgen05.st.sync.aligned.32x32b.x16.b32 [%16], {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15};" ::GK_W8(
+                     r, 0),
+                 GK_W8(r, 8), "r"(addr)
+                 : "memory");
+}
+
+// ---- the walk ----
+
+struct RowsSeq {
+    int q0, q_len, kv;
+    int at;      // position of row 0's token
+    int blocks;  // of 256 rows
+    bool bad;    // longer than its page table
+};
+
+__device__ __forceinline__ RowsSeq rows_seq(const AttendParams &P, uint32_t s)
+{
+    const SeqSpan sp = seq_span(P.seqs, s);
+    RowsSeq w;
+    w.q0 = sp.q0;
+    w.q_len = sp.q_len;
+    w.kv = sp.kv;
+    w.at = sp.kv - sp.q_len;
+    w.blocks = (int)(((uint32_t)sp.q_len * P.G + (kRowsBlock - 1)) / kRowsBlock);
+    w.bad = (uint64_t)sp.kv > (uint64_t)P.seqs.max_pages * P.cache.T;
+    return w;
+}
+
+struct RowsSpan {
+    int lo, hi;  // tokens that some row of the block attends to
+    int first;   // first token of the first tile
+    int tiles;
+};
+
+__device__ __forceinline__ RowsSpan rows_span(const AttendParams &P, const RowsSeq &w, int blk)
+{
+    const int rows = w.q_len * (int)P.G;
+    const int j0 = (int)P.by_G.div((uint32_t)(blk * kRowsBlock));
+    const int j1 = (int)P.by_G.div((uint32_t)min((blk + 1) * kRowsBlock, rows) - 1u);
+    RowsSpan r;
+    r.hi = P.causal ? min(max(0, w.at + j1 + 1), w.kv) : w.kv;
+    r.lo = P.window ? (int)max(0ll, (long long)w.at + j0 + 1 - (long long)P.window) : 0;
+    r.first = r.lo / kRowsTile * kRowsTile;
+    r.tiles = w.bad ? 1 : max(1, (r.hi - r.first + kRowsTile - 1) / kRowsTile);
+    return r;
+}
+
+// Tiles of a sequence for one key head, for each lane its own sequence; the warp helps with long ones.
+__device__ __forceinline__ long long rows_tiles(const AttendParams &P, const RowsSeq &w, int lane)
+{
+    long long n = 0;
+    const bool own = w.blocks <= 4;
+    if (own)
+        for (int b = 0; b < w.blocks; ++b) n += rows_span(P, w, b).tiles;
+    uint32_t rest = __ballot_sync(0xffffffffu, !own);
+    while (rest) {
+        const int src = __ffs(rest) - 1;
+        rest &= rest - 1;
+        RowsSeq o;
+        o.q_len = __shfl_sync(0xffffffffu, w.q_len, src);
+        o.kv = __shfl_sync(0xffffffffu, w.kv, src);
+        o.at = __shfl_sync(0xffffffffu, w.at, src);
+        o.blocks = __shfl_sync(0xffffffffu, w.blocks, src);
+        o.bad = __shfl_sync(0xffffffffu, (int)w.bad, src) != 0;
+        long long m = 0;
+        for (int b = lane; b < o.blocks; b += 32) m += rows_span(P, o, b).tiles;
+#pragma unroll
+        for (int k = 16; k; k >>= 1) m += __shfl_xor_sync(0xffffffffu, m, k);
+        if (lane == src) n = m;
+    }
+    return n;
+}
+
+// A stretch's place in the line, one (block, head) at a time.  Every role walks by itself.
+struct RowsWalk {
+    uint32_t s;
+    RowsSeq w;
+    RowsSpan sp;
+    int blk, h;
+    int t0, t1;   // tiles of the current part
+    int left;     // tiles of the stretch from t0 on
+};
+
+__device__ __forceinline__ bool walk_next(const AttendParams &P, RowsWalk &k)
+{
+    k.left -= k.t1 - k.t0;
+    if (k.left <= 0) return false;
+    k.t0 = 0;
+    if (++k.h == (int)P.cache.H) {
+        k.h = 0;
+        if (++k.blk == k.w.blocks) {
+            k.blk = 0;
+            do {
+                if (++k.s >= P.seqs.n_seqs) return false;
+                k.w = rows_seq(P, k.s);
+            } while (k.w.blocks == 0);
+        }
+        k.sp = rows_span(P, k.w, k.blk);
+    }
+    k.t1 = min(k.sp.tiles, k.left);
+    return true;
+}
+
+struct RowsShared {
+    unsigned long long full[kRowsStages], empty[kRowsStages], q_full[2], s_full[2], p_full[2], o_full[2], scale_full[kRowsScaleSlots];
+    unsigned long long drained;
+    long long total, begin, before;
+    uint32_t seq;
+    int blk, h, tile;
+    uint32_t tmem, abort_flag, beat, last, stop;
+    int bad_lo, bad_hi;  // tokens among which V holds infinities or NaN that not every row may see
+    long long warp_sum[16];
+    long long row_at[2][kRowsTile];  // byte offset of each token of a tile, or -1
+    uint32_t missing[8];             // a page that the table should have held is missing: by part, in turn
+    float ks[kRowsScaleSlots][kRowsTile], vs[kRowsScaleSlots][kRowsTile];
+    float vref[kRowsScaleSlots], vdown[kRowsScaleSlots], vtop[2][4];
+};
+
+__device__ __forceinline__ void named_sync(int id, int threads)
+{
+    asm volatile("bar.sync %0, %1;" ::"r"(id), "r"(threads) : "memory");
+}
+
+__device__ __forceinline__ bool named_and(int id, int threads, bool x)
+{
+    uint32_t r;
+    asm volatile("{ .reg .pred p, q; setp.ne.u32 p, %1, 0; barrier.cta.red.and.aligned.pred q, %2, %3, p; selp.u32 %0, 1, 0, q; }"
+                 : "=r"(r) : "r"((uint32_t)x), "r"(id), "r"(threads) : "memory");
+    return r != 0;
+}
+
+// Offset of 16-byte piece c (8 values) of row r in a tile: 64-value halves one after the other, rows of 128 bytes,
+// pieces exchanged within 8 rows as the hardware's 128-byte swizzle has them.
+__device__ __forceinline__ uint32_t tc_piece(uint32_t r, uint32_t c)
+{
+    return (c >> 3) * (kRowsTile * 128u) + r * 128u + (((c & 7u) ^ (r & 7u)) << 4);
+}
+
+__device__ __forceinline__ void sts16(uint32_t a, uint32_t x, uint32_t y, uint32_t z, uint32_t w)
+{
+    asm volatile("st.shared.v4.b32 [%0], {%1,%2,%3,%4};" ::"r"(a), "r"(x), "r"(y), "r"(z), "r"(w) : "memory");
+}
+
+__device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c)
+{
+    float2 d;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;"
+        : "=l"(*reinterpret_cast<unsigned long long *>(&d))
+        : "l"(*reinterpret_cast<const unsigned long long *>(&a)), "l"(*reinterpret_cast<const unsigned long long *>(&b)),
+          "l"(*reinterpret_cast<const unsigned long long *>(&c)));
+    return d;
+}
+__device__ __forceinline__ float2 mul2(float2 a, float2 b)
+{
+    float2 d;
+    asm("mul.rn.f32x2 %0, %1, %2;"
+        : "=l"(*reinterpret_cast<unsigned long long *>(&d))
+        : "l"(*reinterpret_cast<const unsigned long long *>(&a)), "l"(*reinterpret_cast<const unsigned long long *>(&b)));
+    return d;
+}
+__device__ __forceinline__ float2 add2(float2 a, float2 b)
+{
+    float2 d;
+    asm("add.rn.f32x2 %0, %1, %2;"
+        : "=l"(*reinterpret_cast<unsigned long long *>(&d))
+        : "l"(*reinterpret_cast<const unsigned long long *>(&a)), "l"(*reinterpret_cast<const unsigned long long *>(&b)));
+    return d;
+}
+
+// ---- roles ----
+
+// K and V of the stretch's tiles, in the order K, V, K, V.
+template <bool FP8, int DP>
+__device__ __forceinline__ void rows_load(const RowsParams &R, RowsShared &sh, RowsWalk k, uint32_t smem, int tid)
+{
+    using C = RowsCfg<FP8, DP>;
+    const AttendParams &P = R.a;
+    constexpr int CPR = FP8 ? DP / 16 : DP / 8;          // 16-byte pieces of a cached row
+    constexpr int STEPS = kRowsTile * CPR / 128;         // pieces of a thread
+    const uint32_t pieces = FP8 ? P.cache.D / 16u : P.cache.D / 8u;
+    const int lane = tid & 31, warp = tid >> 5;
+    volatile uint32_t *abort_flag = &sh.abort_flag;
+    uint32_t unit = 0;      // K and V tiles so far
+    uint32_t pending = 0;   // of them, copied but not yet announced
+    uint32_t tile_no = 0, part_no = 0;
+
+    auto announce = [&]() {
+        copy_wait<0>();
+        fence_async_smem();
+        for (; pending; --pending) mbar_arrive(smem_addr(&sh.full[(unit - pending) % kRowsStages]));
+    };
+    auto wait_empty = [&](uint32_t u) -> bool {
+        if (u < kRowsStages) return true;
+        const uint32_t bar = smem_addr(&sh.empty[u % kRowsStages]), parity = (u / kRowsStages - 1u) & 1u;
+        if (mbar_test_wait(bar, parity)) return true;
+        if (!FP8) announce();   // the consumer may need what is in flight before it can free a stage
+        return mbar_wait(bar, parity, abort_flag, R.error, 0x801u, R.wait_limit_ns);
+    };
+
+    uint4 next[FP8 ? STEPS : 1];
+    bool ok = true;
+    do {
+        float vref = 0.f;
+        if (tid == 0) sh.missing[(part_no + 4u) & 7u] = 0u;   // four parts ahead: nobody is there yet
+        for (int t = k.t0; t < k.t1; ++t, ++tile_no) {
+            const int tok = k.sp.first + t * kRowsTile + tid;
+            long long at = -1;
+            bool missing = k.w.bad;
+            float ks = 0.f, vs = 0.f;
+            if (tok >= k.sp.lo && tok < k.sp.hi && !k.w.bad) {
+                const uint32_t page = P.cache.by_T.div((uint32_t)tok);
+                const int g = __ldg(P.seqs.page_table + (uint64_t)k.s * P.seqs.table_stride + page);
+                if ((uint32_t)g < P.cache.num_pages) {
+                    at = (long long)((uint64_t)g * P.cache.page + (uint64_t)((uint32_t)tok - page * P.cache.T) * P.cache.tok +
+                                     (uint64_t)k.h * P.cache.head);
+                    if (FP8) {
+                        ks = __ldg(P.cache.ks + (uint64_t)g * P.cache.s_page + k.h);
+                        vs = __ldg(P.cache.vs + (uint64_t)g * P.cache.s_page + k.h);
+                    }
+                } else {
+                    missing = true;
+                }
+            }
+            sh.row_at[tile_no & 1u][tid] = at;
+            const uint32_t slot = tile_no % kRowsScaleSlots;
+            if (FP8) {
+                float top = fabsf(vs);
+                if (!(top <= 3.402823466e38f)) top = 0.f;
+                top = __uint_as_float(__reduce_max_sync(0xffffffffu, __float_as_uint(top)));
+                if (lane == 0) sh.vtop[tile_no & 1u][warp] = top;
+            }
+            if (missing) {
+                sh.missing[part_no & 7u] = 1u;
+                if (P.seqs.status) P.seqs.status[k.s] = 2;  // GK_JOB_PAGE_TABLE
+            }
+            ok = named_and(2, 128, ok);   // the loaders give up together
+            if (!ok) break;
+            if (FP8) {
+                const float *v = sh.vtop[tile_no & 1u];
+                const float top = fmaxf(fmaxf(v[0], v[1]), fmaxf(v[2], v[3]));
+                const float was = vref;
+                if (top > vref) vref = top;
+                sh.ks[slot][tid] = ks;
+                sh.vs[slot][tid] = vref > 0.f ? vs * (C::kUp / vref) : 0.f;
+                if (tid == 0) {
+                    sh.vref[slot] = vref;
+                    sh.vdown[slot] = was == vref ? 1.f : was / vref;
+                }
+                __syncwarp();
+                if (lane == 0) mbar_arrive(smem_addr(&sh.scale_full[slot]));
+            }
+            const long long *row_at = sh.row_at[tile_no & 1u];
+#pragma unroll
+            for (int kv = 0; kv < 2; ++kv) {
+                const uint8_t *base = kv ? P.cache.v : P.cache.k;
+                if (FP8) {
+#pragma unroll
+                    for (int i = 0; i < STEPS; ++i) {
+                        const uint32_t j = tid + 128u * i, r = j / CPR, c = j % CPR;
+                        const long long off = row_at[r];
+                        next[i] = make_uint4(0u, 0u, 0u, 0u);
+                        if (off >= 0 && c < pieces) next[i] = __ldg(reinterpret_cast<const uint4 *>(base + off + 16u * c));
+                    }
+                }
+                ok = ok && wait_empty(unit);
+                if (!ok) continue;
+                const uint32_t dst = smem + C::KV_OFF + (unit % kRowsStages) * C::TILE_BYTES;
+                if (FP8) {
+#pragma unroll
+                    for (int i = 0; i < STEPS; ++i) {
+                        const uint32_t j = tid + 128u * i, r = j / CPR, c = j % CPR;
+                        const uint4 x = next[i];
+                        sts16(dst + tc_piece(r, 2u * c), e4m3_to_f16(x.x), e4m3_to_f16(x.x >> 16), e4m3_to_f16(x.y), e4m3_to_f16(x.y >> 16));
+                        sts16(dst + tc_piece(r, 2u * c + 1u), e4m3_to_f16(x.z), e4m3_to_f16(x.z >> 16), e4m3_to_f16(x.w), e4m3_to_f16(x.w >> 16));
+                    }
+                    fence_async_smem();
+                    mbar_arrive(smem_addr(&sh.full[unit % kRowsStages]));
+                    ++unit;
+                } else {
+#pragma unroll
+                    for (int i = 0; i < STEPS; ++i) {
+                        const uint32_t j = tid + 128u * i, r = j / CPR, c = j % CPR;
+                        const long long off = row_at[r];
+                        const bool take = off >= 0 && c < pieces;
+                        copy16(dst + tc_piece(r, c), base + (take ? off + 16u * c : 0), take);
+                    }
+                    copy_commit();
+                    ++unit;
+                    ++pending;
+                }
+            }
+        }
+        ++part_no;
+    } while (named_and(2, 128, ok) && walk_next(P, k));
+    announce();
+}
+
+// All MMAs, by one thread.
+template <bool FP8, int DP>
+__device__ __forceinline__ void rows_mma(const RowsParams &R, RowsShared &sh, RowsWalk k, uint32_t smem, uint32_t tmem)
+{
+    using C = RowsCfg<FP8, DP>;
+    const AttendParams &P = R.a;
+    volatile uint32_t *abort_flag = &sh.abort_flag;
+    constexpr uint32_t kS = tc_idesc(FP8, kRowsTile, false), kO = tc_idesc(FP8, DP, true);
+    uint32_t tile_no = 0;
+    uint32_t p_phase[2] = {0, 0}, q_phase[2] = {0, 0};
+    auto wait = [&](unsigned long long *bar, uint32_t parity, uint32_t where) {
+        return mbar_wait(smem_addr(bar), parity, abort_flag, R.error, where, R.wait_limit_ns);
+    };
+    auto add_values = [&](int i, uint32_t n, bool first) {  // O_i += P_i V
+        const uint32_t v = smem + C::KV_OFF + ((2u * n + 1u) % kRowsStages) * C::TILE_BYTES;
+#pragma unroll
+        for (int s = 0; s < kRowsTile / 16; ++s)
+            tc_mma_ts(tmem + 256u + i * 128u, tmem + i * 128u + 8u * s, tc_desc(v + s * 2048u, kRowsTile * 128u), kO, !first || s > 0);
+    };
+    do {
+        const int rows = min(kRowsBlock, k.w.q_len * (int)P.G - k.blk * kRowsBlock);
+        const int act = rows > kRowsTile ? 2 : 1;
+        const int nt = k.t1 - k.t0;
+        for (int t = 0; t <= nt; ++t) {
+            const uint32_t n = tile_no + t, u = 2u * n;  // K's place among the loaded tiles
+            if (t < nt && !wait(&sh.full[u % kRowsStages], (u / kRowsStages) & 1u, 0x811u)) return;
+            if (t > 0 && !wait(&sh.full[(u - 1u) % kRowsStages], ((u - 1u) / kRowsStages) & 1u, 0x812u)) return;
+            for (int i = 0; i < act; ++i) {
+                if (t > 0) {
+                    if (!wait(&sh.p_full[i], p_phase[i] & 1u, 0x813u)) return;
+                    ++p_phase[i];
+                    tc_fence_after();
+                    add_values(i, n - 1u, t == 1);
+                    if (t == nt) tc_commit(smem_addr(&sh.o_full[i]));
+                }
+                if (t < nt) {
+                    if (t == 0) {
+                        if (!wait(&sh.q_full[i], q_phase[i] & 1u, 0x814u)) return;
+                        ++q_phase[i];
+                        tc_fence_after();
+                    }
+                    const uint32_t q = smem + C::Q_OFF + i * C::TILE_BYTES, kk = smem + C::KV_OFF + (u % kRowsStages) * C::TILE_BYTES;
+#pragma unroll
+                    for (int s = 0; s < DP / 16; ++s) {
+                        const uint32_t off = (s >> 2) * (kRowsTile * 128u) + (s & 3) * 32u;
+                        tc_mma_ss(tmem + i * 128u, tc_desc(q + off, 16u), tc_desc(kk + off, 16u), kS, s > 0);
+                    }
+                    tc_commit(smem_addr(&sh.s_full[i]));
+                }
+            }
+            if (t > 0) tc_commit(smem_addr(&sh.empty[(u - 1u) % kRowsStages]));
+            if (t < nt) tc_commit(smem_addr(&sh.empty[u % kRowsStages]));
+        }
+        tile_no += nt;
+    } while (walk_next(P, k));
+}
+
+// This thread's query row into shared memory, as f16 (fp8 caches, divided by a power of two that is returned) or bf16.
+template <bool FP8, int DP>
+__device__ __forceinline__ float rows_query(const RowsParams &R, const RowsWalk &k, uint32_t dst, int r, int row, bool live)
+{
+    const AttendParams &P = R.a;
+    float up = 1.f;
+    const uint32_t j = P.by_G.div((uint32_t)(live ? row : 0));
+    const uint32_t head = (uint32_t)k.h * P.G + (uint32_t)((live ? row : 0) - (int)(j * P.G));
+    const __nv_bfloat16 *p = P.q + (uint64_t)(k.w.q0 + j) * P.q_tok + (uint64_t)head * P.q_head;
+    const uint32_t pieces = P.cache.D / 8u;
+    float down = R.q_sign;
+    if (FP8) {
+        uint32_t top = 0;
+#pragma unroll 4
+        for (uint32_t c = 0; c < DP / 8; ++c) {
+            uint4 x = make_uint4(0u, 0u, 0u, 0u);
+            if (live && c < pieces) x = __ldg(reinterpret_cast<const uint4 *>(p) + c);
+            const uint32_t w[4] = {x.x, x.y, x.z, x.w};
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const uint32_t a = w[e] & 0x7fffu, b = (w[e] >> 16) & 0x7fffu;
+                if (a < 0x7f80u) top = max(top, a);
+                if (b < 0x7f80u) top = max(top, b);
+            }
+        }
+        const int ex = min(max((int)(top >> 7) - 127, -126), 126);
+        down *= __uint_as_float((uint32_t)(127 - ex) << 23);
+        up = __uint_as_float((uint32_t)(127 + ex) << 23);
+    }
+#pragma unroll 4
+    for (uint32_t c = 0; c < DP / 8; ++c) {
+        uint4 x = make_uint4(0u, 0u, 0u, 0u);
+        if (live && c < pieces) x = __ldg(reinterpret_cast<const uint4 *>(p) + c);
+        uint32_t w[4] = {x.x, x.y, x.z, x.w};
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            const float a = __uint_as_float(w[e] << 16) * down, b = __uint_as_float(w[e] & 0xffff0000u) * down;
+            w[e] = FP8 ? f16x2(a, b) : bf16x2(a, b);
+        }
+        sts16(dst + tc_piece(r, c), w[0], w[1], w[2], w[3]);
+    }
+    return up;
+}
+
+// Softmax and output of one tile of 128 rows: one thread per row.
+template <bool FP8, int DP>
+__device__ __forceinline__ void rows_softmax(const RowsParams &R, RowsShared &sh, RowsWalk k, long long begin, long long ctas,
+                                             uint8_t *smem_ptr, uint32_t smem, uint32_t tmem, int i, int tid)
+{
+    using C = RowsCfg<FP8, DP>;
+    const AttendParams &P = R.a;
+    volatile uint32_t *abort_flag = &sh.abort_flag;
+    const int lane = tid & 31, r = tid & 127;
+    const uint32_t my = tmem + ((uint32_t)(r & 96) << 16);   // this warp's lanes
+    const uint32_t s_at = my + i * 128u, o_at = my + 256u + i * 128u;
+    uint32_t tile_no = 0, part_no = 0, s_phase = 0, o_phase = 0;
+    long long place = begin;   // of the current part's first tile in the line
+    bool ok = true;
+    for (;;) {
+        const int rows = min(kRowsBlock, k.w.q_len * (int)P.G - k.blk * kRowsBlock);
+        const int row = k.blk * kRowsBlock + i * kRowsTile + r;   // row of the sequence: token * G + head of the group
+        const bool active = i * kRowsTile < rows;
+        const bool live = i * kRowsTile + r < rows;
+        const int nt = k.t1 - k.t0;
+        const bool whole = k.t0 == 0 && k.t1 == k.sp.tiles;
+        const long long item = place - k.t0;
+        float m = -INFINITY, l = 0.f, vref = 1.f, mul = R.scale_log2;
+        int lo = 0, hi = 0;
+        // tokens that every live row of this tile attends to: [all_lo, all_hi)
+        int all_lo = 0, all_hi = 0;
+        if (active && (P.causal || P.window)) {
+            const int p0 = k.w.at + (int)P.by_G.div((uint32_t)(k.blk * kRowsBlock + i * kRowsTile));
+            const int p1 = k.w.at + (int)P.by_G.div((uint32_t)(k.blk * kRowsBlock + min(rows, (i + 1) * kRowsTile) - 1));
+            all_hi = P.causal ? min(max(0, p0 + 1), k.w.kv) : k.w.kv;
+            all_lo = P.window ? (int)max(0ll, (long long)p1 + 1 - (long long)P.window) : 0;
+        } else {
+            all_hi = k.w.kv;
+        }
+        if (tid == 0) {
+            sh.bad_lo = 0x7fffffff;
+            sh.bad_hi = 0;
+            sh.stop = *abort_flag;
+        }
+        named_sync(1, 256);
+        if (sh.stop) return;   // both tiles' threads together
+        if (active) {
+            if (live) {
+                const int pos = k.w.at + (int)P.by_G.div((uint32_t)row);
+                hi = P.causal ? min(max(0, pos + 1), k.w.kv) : k.w.kv;
+                lo = P.window ? (int)max(0ll, (long long)pos + 1 - (long long)P.window) : 0;
+            }
+            mul *= rows_query<FP8, DP>(R, k, smem + C::Q_OFF + i * C::TILE_BYTES, r, row, live);
+            fence_async_smem();
+            __syncwarp();
+            if (lane == 0) mbar_arrive(smem_addr(&sh.q_full[i]));
+            float2 sum = make_float2(0.f, 0.f);
+            for (int t = 0; t < nt; ++t) {
+                const uint32_t n = tile_no + t;
+                const int tok0 = k.sp.first + (k.t0 + t) * kRowsTile;
+                ok = mbar_wait(smem_addr(&sh.s_full[i]), s_phase & 1u, abort_flag, R.error, 0x821u, R.wait_limit_ns);
+                ++s_phase;
+                if (!__all_sync(0xffffffffu, ok)) {
+                    ok = false;
+                    break;
+                }
+                tc_fence_after();
+                uint32_t raw[128];
+#pragma unroll
+                for (int c = 0; c < 4; ++c) tc_ld32(raw + 32 * c, s_at + 32u * c);
+                tc_wait_ld();
+                float2 *s = reinterpret_cast<float2 *>(raw);
+                const uint32_t slot = n % kRowsScaleSlots;
+                float down_v = 1.f;
+                if (FP8) {
+                    mbar_wait(smem_addr(&sh.scale_full[slot]), (n / kRowsScaleSlots) & 1u, abort_flag, R.error, 0x822u, R.wait_limit_ns);
+                    const float2 *ks = reinterpret_cast<const float2 *>(sh.ks[slot]);
+#pragma unroll
+                    for (int c = 0; c < 64; ++c) s[c] = mul2(s[c], ks[c]);
+                    vref = sh.vref[slot];
+                    down_v = sh.vdown[slot];
+                }
+                if (__any_sync(0xffffffffu, tok0 < lo || tok0 + kRowsTile > hi)) {
+#pragma unroll
+                    for (int c = 0; c < 128; ++c)
+                        if (tok0 + c < lo || tok0 + c >= hi) raw[c] = 0xff800000u;
+                }
+                if (tok0 < all_lo || min(tok0 + kRowsTile, k.sp.hi) > all_hi) {
+                    // 0 * infinity must not reach rows that do not attend to a token: such V are set to 0 here and added
+                    // to the rows that do in the end
+                    const uint32_t vu = 2u * n + 1u;
+                    mbar_wait(smem_addr(&sh.full[vu % kRowsStages]), (vu / kRowsStages) & 1u, abort_flag, R.error, 0x823u, R.wait_limit_ns);
+                    uint8_t *v = smem_ptr + C::KV_OFF + (vu % kRowsStages) * C::TILE_BYTES;
+                    bool found = false;
+                    for (int c = r; c < C::TILE_BYTES / 16; c += 128) {
+                        uint32_t *w = reinterpret_cast<uint32_t *>(v + 16 * c);
+                        const uint4 x = *reinterpret_cast<const uint4 *>(w);
+                        const uint32_t y[4] = {x.x, x.y, x.z, x.w};
+                        constexpr uint32_t E = FP8 ? 0x7c00u : 0x7f80u;
+                        bool hit = false;
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) hit |= (y[e] & E) == E || (y[e] & (E << 16)) == (E << 16);
+                        if (hit) {
+                            found = true;
+                            atomicMin(&sh.bad_lo, tok0);
+                            atomicMax(&sh.bad_hi, tok0 + kRowsTile);
+                            __threadfence_block();
+#pragma unroll
+                            for (int e = 0; e < 4; ++e) {
+                                uint32_t z = y[e];
+                                if ((z & E) == E) z &= 0xffff0000u;
+                                if ((z & (E << 16)) == (E << 16)) z &= 0xffffu;
+                                w[e] = z;
+                            }
+                        }
+                    }
+                    if (found) fence_async_smem();
+                }
+                float top = -INFINITY;
+#pragma unroll
+                for (int c = 0; c < 128; c += 2) top = fmaxf(top, fmaxf(s[c / 2].x, s[c / 2].y));
+                const float x = top * mul;
+                if (t == 0) {
+                    m = top == -INFINITY ? -INFINITY : x;
+                } else if (__any_sync(0xffffffffu, x > m + C::kRise || (FP8 && down_v != 1.f))) {
+                    const float nm = top == -INFINITY ? m : fmaxf(m, x);
+                    const float f = nm == m ? 1.f : fast_exp2(m - nm);
+                    m = nm;
+                    sum.x *= f;
+                    sum.y *= f;
+                    const float g = f * down_v;
+                    uint32_t o[32];
+#pragma unroll
+                    for (int c = 0; c < DP / 32; ++c) {
+                        tc_ld32(o, o_at + 32u * c);
+                        tc_wait_ld();
+#pragma unroll
+                        for (int e = 0; e < 32; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * g);
+                        tc_st32(o_at + 32u * c, o);
+                    }
+                }
+                const float ref = m == -INFINITY ? 0.f : -m;
+                const float2 mul_2 = make_float2(mul, mul), ref_2 = make_float2(ref, ref);
+#pragma unroll
+                for (int c4 = 0; c4 < 4; ++c4) {
+                    uint32_t pk[16];
+#pragma unroll
+                    for (int c = 0; c < 16; ++c) {
+                        float2 e = fma2(s[16 * c4 + c], mul_2, ref_2);
+                        e.x = fast_exp2(e.x);
+                        e.y = fast_exp2(e.y);
+                        sum = add2(sum, e);
+                        if (FP8) {
+                            const float2 v = reinterpret_cast<const float2 *>(sh.vs[slot])[16 * c4 + c];
+                            const float2 w = mul2(e, v);
+                            // a masked token stays 0 whatever its scale is
+                            pk[c] = f16x2(e.x == 0.f ? 0.f : w.x, e.y == 0.f ? 0.f : w.y);
+                        } else {
+                            pk[c] = bf16x2(e.x, e.y);
+                        }
+                    }
+                    tc_st16(s_at + 16u * c4, pk);
+                }
+                tc_wait_st();
+                tc_fence_before();
+                __syncwarp();
+                if (lane == 0) mbar_arrive(smem_addr(&sh.p_full[i]));
+            }
+            l = sum.x + sum.y;
+        }
+        float *part = P.parts + (uint64_t)(2u * blockIdx.x + (k.t0 > 0 ? 0u : 1u)) * C::PART_FLOATS;
+        const int prow = i * kRowsTile + r;
+        if (active && ok) {
+            ok = mbar_wait(smem_addr(&sh.o_full[i]), o_phase & 1u, abort_flag, R.error, 0x824u, R.wait_limit_ns);
+            ++o_phase;
+            ok = __all_sync(0xffffffffu, ok);
+        }
+        named_sync(1, 256);   // both tiles are through: bad_lo and bad_hi are final
+        const uint32_t j = P.by_G.div((uint32_t)(live ? row : 0));
+        const uint32_t head = (uint32_t)k.h * P.G + (uint32_t)((live ? row : 0) - (int)(j * P.G));
+        __nv_bfloat16 *out = P.out + (uint64_t)(k.w.q0 + j) * P.o_tok + (uint64_t)head * P.o_head;
+        if (active && ok) {
+            tc_fence_after();
+            if (sh.missing[part_no & 7u]) l = __int_as_float(0x7fc00000);
+            const int bad_lo = max(sh.bad_lo, lo), bad_hi = min(sh.bad_hi, hi);
+            const float back = FP8 ? vref * (1.f / C::kUp) : 1.f;
+            const float inv = !whole ? back : l == 0.f ? 0.f : back / l;
+#pragma unroll 1
+            for (int c = 0; c < DP / 32; ++c) {
+                uint32_t o[32];
+                __syncwarp();
+                tc_ld32(o, o_at + 32u * c);
+                tc_wait_ld();
+                if (live) {
+                    for (int t = bad_lo; t < bad_hi; ++t) {   // infinities and NaN that the products left out
+                        const uint32_t page = P.cache.by_T.div((uint32_t)t);
+                        const int g = __ldg(P.seqs.page_table + (uint64_t)k.s * P.seqs.table_stride + page);
+                        if ((uint32_t)g >= P.cache.num_pages) continue;
+                        const uint8_t *v = P.cache.v + (uint64_t)g * P.cache.page + (uint64_t)((uint32_t)t - page * P.cache.T) * P.cache.tok +
+                                           (uint64_t)k.h * P.cache.head;
+#pragma unroll
+                        for (int e = 0; e < 32; ++e) {
+                            const int d = 32 * c + e;
+                            if (d >= (int)P.cache.D) continue;
+                            const float y = FP8 ? __half2float(__half(__nv_cvt_fp8_to_halfraw(v[d], __NV_E4M3)))
+                                                : __bfloat162float(reinterpret_cast<const __nv_bfloat16 *>(v)[d]);
+                            if (!(fabsf(y) <= 3.402823466e38f)) o[e] = __float_as_uint(__uint_as_float(o[e]) + y);
+                        }
+                    }
+#pragma unroll
+                    for (int e = 0; e < 32; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * inv);
+                    if (whole) {
+#pragma unroll
+                        for (int e = 0; e < 32; e += 8)
+                            if (32 * c + e < (int)P.cache.D) {
+                                const float *f = reinterpret_cast<const float *>(o) + e;
+                                *reinterpret_cast<uint4 *>(out + 32 * c + e) =
+                                    make_uint4(bf16x2(f[0], f[1]), bf16x2(f[2], f[3]), bf16x2(f[4], f[5]), bf16x2(f[6], f[7]));
+                            }
+                    } else {
+#pragma unroll
+                        for (int e = 0; e < 32; e += 4)
+                            *reinterpret_cast<uint4 *>(part + (size_t)((32 * c + e) / 4 * kRowsBlock + prow) * 4) =
+                                make_uint4(o[e], o[e + 1], o[e + 2], o[e + 3]);
+                    }
+                }
+            }
+            if (live) {
+                if (whole) {
+                    if (P.lse) P.lse[(uint64_t)(k.w.q0 + j) * P.Hq + head] = l == 0.f ? -INFINITY : m * 0.69314718055994531f + logf(l);
+                } else {
+                    part[kRowsBlock * DP + prow] = m;
+                    part[kRowsBlock * (DP + 1) + prow] = l;
+                }
+            }
+            tc_fence_before();
+        }
+        if (!whole) {
+            // the CTAs that share the block: those whose stretches hold its first and its last tile
+            const uint32_t c0 = (uint32_t)(((item + 1) * ctas - 1) / sh.total);
+            const uint32_t c1 = (uint32_t)(((item + k.sp.tiles) * ctas - 1) / sh.total);
+            __threadfence();
+            named_sync(1, 256);
+            if (tid == 0) {
+                const uint32_t seen = atomicAdd(P.counters + c0, 1u);
+                sh.last = seen == c1 - c0;
+                if (seen == c1 - c0) P.counters[c0] = 0u;  // ready for the next call
+            }
+            named_sync(1, 256);
+            if (sh.last && live) {
+                __threadfence();
+                float jm = -INFINITY;
+                for (uint32_t c = c0; c <= c1; ++c)
+                    jm = fmaxf(jm, __ldcg(P.parts + (uint64_t)(2u * c + (c == c0 ? 1u : 0u)) * C::PART_FLOATS + kRowsBlock * DP + prow));
+                const float ref = jm == -INFINITY ? 0.f : jm;
+                float jl = 0.f;
+#pragma unroll 1
+                for (int d = 0; d < (int)P.cache.D; d += 16) {
+                    float4 v[4] = {};
+                    jl = 0.f;
+                    for (uint32_t c = c0; c <= c1; ++c) {
+                        const float *p = P.parts + (uint64_t)(2u * c + (c == c0 ? 1u : 0u)) * C::PART_FLOATS;
+                        const float f = fast_exp2(__ldcg(p + kRowsBlock * DP + prow) - ref);
+                        jl += f * __ldcg(p + kRowsBlock * (DP + 1) + prow);
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) {
+                            const float4 y = __ldcg(reinterpret_cast<const float4 *>(p + (size_t)((d / 4 + e) * kRowsBlock + prow) * 4));
+                            v[e].x += f * y.x;
+                            v[e].y += f * y.y;
+                            v[e].z += f * y.z;
+                            v[e].w += f * y.w;
+                        }
+                    }
+                    const float inv = jl == 0.f ? 0.f : 1.f / jl;
+#pragma unroll
+                    for (int e = 0; e < 4; e += 2)
+                        *reinterpret_cast<uint4 *>(out + d + 4 * e) =
+                            make_uint4(bf16x2(v[e].x * inv, v[e].y * inv), bf16x2(v[e].z * inv, v[e].w * inv),
+                                       bf16x2(v[e + 1].x * inv, v[e + 1].y * inv), bf16x2(v[e + 1].z * inv, v[e + 1].w * inv));
+                }
+                if (P.lse) P.lse[(uint64_t)(k.w.q0 + j) * P.Hq + head] = jl == 0.f ? -INFINITY : jm * 0.69314718055994531f + logf(jl);
+            }
+        }
+        tile_no += nt;
+        place += nt;
+        ++part_no;
+        if (!walk_next(P, k)) return;
+    }
+}
+
+template <bool FP8, int DP>
+__global__ void __launch_bounds__(kRowsThreads, 1) attend_rows_kernel(const RowsParams R)
+{
+    using C = RowsCfg<FP8, DP>;
+    const AttendParams &P = R.a;
+    extern __shared__ uint8_t smem_raw[];
+    __shared__ RowsShared sh;
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+    uint8_t *smem_ptr = smem_raw + ((1024u - (smem_addr(smem_raw) & 1023u)) & 1023u);
+    const uint32_t smem = smem_addr(smem_ptr);
+
+    // the length of the line of tiles
+    long long total = 0;
+    for (uint32_t s0 = 0; s0 < P.seqs.n_seqs; s0 += kRowsThreads) {
+        const uint32_t s = s0 + tid;
+        RowsSeq w{};
+        if (s < P.seqs.n_seqs) w = rows_seq(P, s);
+        long long n = rows_tiles(P, w, lane) * P.cache.H;
+#pragma unroll
+        for (int o = 16; o; o >>= 1) n += __shfl_xor_sync(0xffffffffu, n, o);
+        if (lane == 0) sh.warp_sum[warp] = n;
+        __syncthreads();
+        for (int i = 0; i < kRowsThreads / 32; ++i) total += sh.warp_sum[i];
+        __syncthreads();
+    }
+    if (total == 0) return;
+    const long long ctas = total < (long long)gridDim.x ? total : (long long)gridDim.x;
+    if ((long long)blockIdx.x >= ctas) return;
+    const long long begin = total * blockIdx.x / ctas, end = total * (blockIdx.x + 1) / ctas;
+
+    // the sequence that the stretch begins in
+    long long before = 0;
+    for (uint32_t s0 = 0; s0 < P.seqs.n_seqs; s0 += kRowsThreads) {
+        const uint32_t s = s0 + tid;
+        RowsSeq w{};
+        if (s < P.seqs.n_seqs) w = rows_seq(P, s);
+        const long long n = rows_tiles(P, w, lane) * P.cache.H;
+        long long incl = n;
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) {
+            const long long x = __shfl_up_sync(0xffffffffu, incl, o);
+            if (lane >= o) incl += x;
+        }
+        if (lane == 31) sh.warp_sum[warp] = incl;
+        __syncthreads();
+        long long base = before;
+        for (int i = 0; i < warp; ++i) base += sh.warp_sum[i];
+        const long long at = base + incl - n;
+        if (n > 0 && begin >= at && begin < at + n) {
+            sh.seq = s;
+            sh.before = at;
+        }
+        for (int i = 0; i < kRowsThreads / 32; ++i) before += sh.warp_sum[i];
+        __syncthreads();
+        if (before > begin) break;
+    }
+    // ... and the block and head within it
+    if (warp == 0) {
+        const RowsSeq w = rows_seq(P, sh.seq);
+        long long off = begin - sh.before;
+        for (int b0 = 0; b0 < w.blocks; b0 += 32) {
+            const int b = b0 + lane;
+            const long long n = b < w.blocks ? (long long)rows_span(P, w, b).tiles * P.cache.H : 0;
+            long long incl = n;
+#pragma unroll
+            for (int o = 1; o < 32; o <<= 1) {
+                const long long x = __shfl_up_sync(0xffffffffu, incl, o);
+                if (lane >= o) incl += x;
+            }
+            const bool here = off >= incl - n && off < incl;
+            if (here) {
+                const long long in = off - (incl - n);
+                const int tiles = rows_span(P, w, b).tiles;
+                sh.blk = b;
+                sh.h = (int)(in / tiles);
+                sh.tile = (int)(in % tiles);
+            }
+            if (__any_sync(0xffffffffu, here)) break;
+            off -= __shfl_sync(0xffffffffu, incl, 31);
+        }
+    }
+    if (tid == 0) {
+        for (int i = 0; i < kRowsStages; ++i) {
+            mbar_init(smem_addr(&sh.full[i]), 128);
+            mbar_init(smem_addr(&sh.empty[i]), 1);
+        }
+        for (int i = 0; i < 2; ++i) {
+            mbar_init(smem_addr(&sh.q_full[i]), 4);
+            mbar_init(smem_addr(&sh.s_full[i]), 1);
+            mbar_init(smem_addr(&sh.p_full[i]), 4);
+            mbar_init(smem_addr(&sh.o_full[i]), 1);
+        }
+        for (int i = 0; i < kRowsScaleSlots; ++i) mbar_init(smem_addr(&sh.scale_full[i]), 4);
+        mbar_init(smem_addr(&sh.drained), 1);
+        sh.abort_flag = 0u;
+        for (int i = 0; i < 8; ++i) sh.missing[i] = 0u;
+        sh.total = total;
+        fence_mbar_init();
+    }
+    if (warp == 12) {
+        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], 512;" ::"r"(smem_addr(&sh.tmem)) : "memory");
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+        tc_fence_before();
+    }
+    __syncthreads();
+    tc_fence_after();
+    const uint32_t tmem = sh.tmem;
+
+    RowsWalk k;
+    k.s = sh.seq;
+    k.w = rows_seq(P, k.s);
+    k.blk = sh.blk;
+    k.h = sh.h;
+    k.sp = rows_span(P, k.w, k.blk);
+    k.left = (int)(end - begin);
+    k.t0 = sh.tile;
+    k.t1 = min(k.sp.tiles, k.t0 + k.left);
+
+    if (warp < 8) {
+        asm volatile("setmaxnreg.inc.sync.aligned.u32 184;");
+        rows_softmax<FP8, DP>(R, sh, k, begin, ctas, smem_ptr, smem, tmem, warp >> 2, tid);
+    } else if (warp < 12) {
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 96;");
+        rows_load<FP8, DP>(R, sh, k, smem, tid - 256);
+    } else {
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 48;");
+        if (tid == 12 * 32) {
+            rows_mma<FP8, DP>(R, sh, k, smem, tmem);
+            // whatever has been issued ends before the tensor memory is given back
+            tc_commit(smem_addr(&sh.drained));
+            mbar_drain(smem_addr(&sh.drained), 0u, 4ull * R.wait_limit_ns);
+        }
+        __syncwarp();
+    }
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    if (warp == 12) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, 512;" ::"r"(tmem) : "memory");
+}
+
+}  // namespace gk

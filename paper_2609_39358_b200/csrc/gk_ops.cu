@@ -6,6 +6,7 @@
 
 #include "gk_append.cuh"
 #include "gk_attend.cuh"
+#include "gk_attend_rows.cuh"
 
 using namespace gk;
 
@@ -105,7 +106,9 @@ int ensure_attention(gk_ctx *c)
 {
     if (c->d_attn) return GK_OK;
     const size_t part = (size_t)(kAttendRows * 256 + 2 * kAttendRows) * 4;
-    const size_t bytes = kAttnCounterBytes + 2 * (size_t)kAttnMaxCtas * part;
+    const size_t few = 2 * (size_t)kAttnMaxCtas * part;
+    const size_t many = 2 * (size_t)c->sm_count * RowsCfg<false, 128>::PART_FLOATS * 4;
+    const size_t bytes = kAttnCounterBytes + (few > many ? few : many);
     if (cudaMalloc(&c->d_attn, bytes) != cudaSuccess) {
         cudaGetLastError();
         c->d_attn = nullptr;
@@ -136,6 +139,25 @@ int launch_attend(gk_ctx *c, const AttendParams &P, cudaStream_t st)
     int grid = c->sm_count * occ;
     if (grid > kAttnMaxCtas) grid = kAttnMaxCtas;
     attend_kernel<FP8, DP><<<grid, kAttendThreads, C::SMEM, st>>>(P);
+    GK_CUDA(c, cudaGetLastError());
+    c->stats.kernels_launched++;
+    return GK_OK;
+}
+
+template <bool FP8, int DP>
+int launch_rows(gk_ctx *c, const RowsParams &P, cudaStream_t st)
+{
+    using C = RowsCfg<FP8, DP>;
+    static bool ready = false;
+    if (!ready) {
+        cudaFuncAttributes a{};
+        GK_CUDA(c, cudaFuncGetAttributes(&a, attend_rows_kernel<FP8, DP>));
+        // the warp roles' shares of the registers add up to 128 a thread, which the launch has to bring along
+        if (a.numRegs < 128) return fail(c, GK_ERR_CUDA, "attend_rows_kernel was built with %d registers", a.numRegs);
+        GK_CUDA(c, cudaFuncSetAttribute(attend_rows_kernel<FP8, DP>, cudaFuncAttributeMaxDynamicSharedMemorySize, C::SMEM));
+        ready = true;
+    }
+    attend_rows_kernel<FP8, DP><<<c->sm_count, kRowsThreads, C::SMEM, st>>>(P);
     GK_CUDA(c, cudaGetLastError());
     c->stats.kernels_launched++;
     return GK_OK;
@@ -229,6 +251,17 @@ int gk_attention(gk_ctx *c, const gk_cache *cache, uint32_t layer, const gk_batc
     P.parts = (float *)(c->d_attn + kAttnCounterBytes);
     const cudaStream_t st = (cudaStream_t)stream;
     const uint32_t D = c->geom.head_dim;
+    const uint32_t max_q = batch->q_start ? (batch->max_q_len ? batch->max_q_len : batch->n_tokens) : 1u;
+    if ((uint64_t)max_q * P.G > kAttendRows && D <= 128) {
+        RowsParams R{};
+        R.a = P;
+        R.scale_log2 = scale == 0.f ? 1.f : fabsf(P.scale_log2);
+        R.q_sign = scale == 0.f ? 0.f : scale < 0.f ? -1.f : 1.f;
+        R.error = c->d_error;
+        R.wait_limit_ns = c->wait_limit_ns;
+        if (c->geom.dtype == GK_FP8_E4M3) return D <= 64 ? launch_rows<true, 64>(c, R, st) : launch_rows<true, 128>(c, R, st);
+        return D <= 64 ? launch_rows<false, 64>(c, R, st) : launch_rows<false, 128>(c, R, st);
+    }
     if (c->geom.dtype == GK_FP8_E4M3)
         return D <= 64 ? launch_attend<true, 64>(c, P, st) : D <= 128 ? launch_attend<true, 128>(c, P, st)
                                                                     : launch_attend<true, 256>(c, P, st);
