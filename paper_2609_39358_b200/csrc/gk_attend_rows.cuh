@@ -13,12 +13,16 @@
 // last fixed (the weights then reach 2^kRise, which neither P's type nor the fp32 sums mind); after the first
 // tiles of a row that is rare.
 //
-// Warps: 0-3 and 4-7 softmax and output of the two tiles, 8-11 load K and V through the page table (bf16:
-// 16-byte asynchronous copies; fp8: loads, conversion to f16, shared-memory stores), 12 issues the MMAs.
+// Warps: 0-3 and 4-7 softmax and output of the two tiles, 12 issues the MMAs, 13 fetches K and V through the page
+// table with one tensor copy (TMA) per page and 128 bytes of a row: bf16 straight into the operand tiles, fp8 into a
+// ring of its own, from which warps 8-11 convert to f16.  Pages that do not tile 128 tokens (or whose rows are not 64 or
+// 128 values) are loaded by warps 8-11 alone, row by row.
 //
 // Work is dealt out as in attend_kernel: the token tiles of all blocks lie in one line, every CTA takes an equal
 // stretch, parts of a block meet in the workspace.
 #pragma once
+
+#include <cuda.h>  // CUtensorMap
 
 #include "gk_attend.cuh"
 #include "gk_device.cuh"
@@ -28,11 +32,26 @@ namespace gk {
 constexpr int kRowsTile = 128;               // query rows of a tile, tokens of a tile
 constexpr int kRowsBlock = 2 * kRowsTile;
 constexpr int kRowsThreads = 512;
-constexpr int kRowsStages = 4;               // K and V tiles in shared memory, taken in turn: K, V, K, V
+constexpr int kRowsRaw = 3;                  // fp8 tiles in flight
 constexpr int kRowsScaleSlots = 4;
+constexpr int kRowsPartSlots = 16;           // more than the parts between the first and the last role
+
+// A block that more than kRowsHere CTAs share: joined by a kernel of its own.
+struct RowsJoin {
+    uint32_t parts;  // 0: none
+    uint32_t s;
+    int blk, h;
+};
+constexpr uint32_t kRowsHere = 4;
 
 struct RowsParams {
+    CUtensorMap map;      // the layer's K and V: dimension, token, head (token and head as they lie), page, K or V
+    uint32_t tma;         // the map is to be used
+    uint32_t head_first;  // the map's second dimension is the head
+    uint32_t per_tile;    // pages of a tile
+    uint32_t page_rows;   // tokens of a page that one copy takes: min(page_tokens, 128)
     AttendParams a;
+    RowsJoin *join;       // one per CTA; null: every block is joined by the CTA that ends last
     float scale_log2;     // |scale| * log2(e); the sign goes into the queries
     float q_sign;         // 1, -1, or 0 with a scale of 0
     uint32_t *error;
@@ -45,7 +64,10 @@ struct RowsCfg {
     static constexpr int TILE_BYTES = kRowsTile * DP * 2;
     static constexpr int Q_OFF = 0;
     static constexpr int KV_OFF = 2 * TILE_BYTES;
-    static constexpr int END = KV_OFF + kRowsStages * TILE_BYTES;
+    static constexpr int STAGES = FP8 ? 3 : 4;                // operand tiles of K and V, taken in turn: K, V, K, V
+    static constexpr int RAW_OFF = KV_OFF + STAGES * TILE_BYTES;
+    static constexpr int RAW_BYTES = FP8 ? kRowsTile * DP : 0;
+    static constexpr int END = RAW_OFF + kRowsRaw * RAW_BYTES;
     static constexpr int SMEM = END + 1024;                   // room to align the tiles
     static constexpr int PART_FLOATS = kRowsBlock * (DP + 2);
     static constexpr float kRise = FP8 ? 4.f : 8.f;
@@ -104,12 +126,11 @@ __device__ __forceinline__ void tc_ld32(uint32_t *r, uint32_t addr)
                  : GK_R8(r, 0), GK_R8(r, 8), GK_R8(r, 16), GK_R8(r, 24)
                  : "r"(addr));
 }
-__device__ __forceinline__ void tc_st32(uint32_t addr, const uint32_t *r)
+__device__ __forceinline__ void tc_ld16(uint32_t *r, uint32_t addr)
 {
-    asm volatile("tcgen05.st.sync.aligned.32x32b.x32.b32 [%32], {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,"
-                 "%16,%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31};" ::GK_W8(r, 0), GK_W8(r, 8), GK_W8(r, 16),
-                 GK_W8(r, 24), "r"(addr)
-                 : "memory");
+    asm volatile("tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15}, [%16];"
+                 : GK_R8(r, 0), GK_R8(r, 8)
+                 : "r"(addr));
 }
 __device__ __forceinline__ void tc_st16(uint32_t addr, const uint32_t *r)
 {
@@ -216,17 +237,30 @@ __device__ __forceinline__ bool walk_next(const AttendParams &P, RowsWalk &k)
     return true;
 }
 
+// What the softmax warps know of a part: written by a warp of its own, one part ahead.
+struct RowsPart {
+    uint32_t s;
+    int q0, at, kv;        // of the sequence
+    int blk, h, rows;      // live rows of the block
+    int first, lo, hi;     // first token of the part's first tile; tokens that some row attends to
+    int tiles;             // of the part
+    bool whole, starts;    // the part is the whole block; it holds the block's first tile
+    uint32_t c0, c1;       // CTAs that share the block
+    bool end;
+};
+
 struct RowsShared {
-    unsigned long long full[kRowsStages], empty[kRowsStages], q_full[2], s_full[2], p_full[2], o_full[2], scale_full[kRowsScaleSlots];
+    unsigned long long full[4], empty[4], raw_full[kRowsRaw], raw_empty[kRowsRaw], q_full[2], s_full[2], p_full[2], o_full[2], scale_full[kRowsScaleSlots];
     unsigned long long drained;
     long long total, begin, before;
     uint32_t seq;
     int blk, h, tile;
-    uint32_t tmem, abort_flag, beat, last, stop;
+    uint32_t tmem, abort_flag, beat, last;
+    RowsPart part[2];
     int bad_lo, bad_hi;  // tokens among which V holds infinities or NaN that not every row may see
     long long warp_sum[16];
     long long row_at[2][kRowsTile];  // byte offset of each token of a tile, or -1
-    uint32_t missing[8];             // a page that the table should have held is missing: by part, in turn
+    uint32_t missing[kRowsPartSlots];             // a page that the table should have held is missing: by part, in turn
     float ks[kRowsScaleSlots][kRowsTile], vs[kRowsScaleSlots][kRowsTile];
     float vref[kRowsScaleSlots], vdown[kRowsScaleSlots], vtop[2][4];
 };
@@ -284,7 +318,170 @@ __device__ __forceinline__ float2 add2(float2 a, float2 b)
 
 // ---- roles ----
 
-// K and V of the stretch's tiles, in the order K, V, K, V.
+__device__ __forceinline__ void mark_missing(const AttendParams &P, RowsShared &sh, uint32_t part, uint32_t s)
+{
+    sh.missing[part % kRowsPartSlots] = 1u;
+    if (P.seqs.status) P.seqs.status[s] = 2;  // GK_JOB_PAGE_TABLE
+}
+
+// A place in the stretch, tile by tile.
+struct RowsAt {
+    RowsWalk k;
+    int t;
+    uint32_t part;
+    bool more;
+};
+
+__device__ __forceinline__ void at_next(const AttendParams &P, RowsAt &a)
+{
+    if (++a.t < a.k.t1) return;
+    a.more = walk_next(P, a.k);
+    a.t = a.k.t0;
+    ++a.part;
+}
+
+// One warp: K and V of the stretch's tiles by tensor copies, a page and 128 bytes of a row each; a lane per page.
+template <bool FP8, int DP>
+__device__ __forceinline__ void rows_fetch(const RowsParams &R, RowsShared &sh, const RowsWalk &k, uint32_t smem, int lane)
+{
+    using C = RowsCfg<FP8, DP>;
+    const AttendParams &P = R.a;
+    volatile uint32_t *abort_flag = &sh.abort_flag;
+    constexpr uint32_t RING = FP8 ? kRowsRaw : C::STAGES;
+    constexpr int PIECES = FP8 ? 1 : DP / 64;
+    RowsAt a{k, k.t0, 0u, true};
+    // the page of this lane in the tile at `a`, or -1
+    auto look_up = [&](const RowsAt &a) -> int {
+        const int tok = a.k.sp.first + a.t * kRowsTile + lane * (int)R.page_rows;
+        if (!a.more || lane >= (int)R.per_tile || tok >= a.k.sp.hi || tok + (int)R.page_rows <= a.k.sp.lo || a.k.w.bad) return -1;
+        return __ldg(P.seqs.page_table + (uint64_t)a.k.s * P.seqs.table_stride + P.cache.by_T.div((uint32_t)tok));
+    };
+    auto wanted = [&](const RowsAt &a) {
+        const int tok = a.k.sp.first + a.t * kRowsTile + lane * (int)R.page_rows;
+        return lane < (int)R.per_tile && tok < a.k.sp.hi && tok + (int)R.page_rows > a.k.sp.lo;
+    };
+    int id = look_up(a);
+    uint32_t last_part = 0xffffffffu;
+    for (uint32_t unit = 0; a.more;) {
+        if (a.part != last_part) {
+            last_part = a.part;
+            if (lane == 0) sh.missing[(a.part + kRowsPartSlots / 2) % kRowsPartSlots] = 0u;
+        }
+        const bool have = (uint32_t)id < P.cache.num_pages;
+        if (wanted(a) && !have) mark_missing(P, sh, a.part, a.k.s);
+        const uint32_t bytes = (uint32_t)__popc(__ballot_sync(0xffffffffu, have)) * R.page_rows * (FP8 ? DP : DP * 2);
+        const int tok0 = a.k.sp.first + a.t * kRowsTile;
+        const int row = R.per_tile == 1u ? tok0 - (int)(P.cache.by_T.div((uint32_t)tok0) * P.cache.T) : 0;
+        const int h = a.k.h, page = id;
+        at_next(P, a);
+        id = look_up(a);
+#pragma unroll
+        for (int kv = 0; kv < 2; ++kv, ++unit) {
+            const uint32_t stage = unit % RING;
+            const uint32_t full = smem_addr(FP8 ? &sh.raw_full[stage] : &sh.full[stage]);
+            bool free = unit < RING;
+            if (!free)
+                free = mbar_wait(smem_addr(FP8 ? &sh.raw_empty[stage] : &sh.empty[stage]), (unit / RING - 1u) & 1u, abort_flag, R.error,
+                                 0x801u, R.wait_limit_ns);
+            if (!__all_sync(0xffffffffu, free)) {
+                // given up: what is in flight lands before the CTA ends
+                for (uint32_t u = unit < RING ? 0u : unit - RING; u < unit; ++u)
+                    mbar_drain(smem_addr(FP8 ? &sh.raw_full[u % RING] : &sh.full[u % RING]), (u / RING) & 1u, R.wait_limit_ns);
+                return;
+            }
+            __syncwarp();
+            if (lane == 0) mbar_arrive_expect_tx(full, bytes);
+            __syncwarp();
+            if (have) {
+                const uint32_t dst = smem + (FP8 ? C::RAW_OFF + stage * C::RAW_BYTES : C::KV_OFF + stage * C::TILE_BYTES) +
+                                     (uint32_t)lane * R.page_rows * (FP8 ? DP : 128u);
+#pragma unroll
+                for (int p = 0; p < PIECES; ++p)
+                    asm volatile("cp.async.bulk.tensor.5d.shared::cta.global.tile.mbarrier::complete_tx::bytes [%0], "
+                                 "[%1, {%2, %3, %4, %5, %6}], [%7];" ::"r"(dst + p * kRowsTile * 128),
+                                 "l"(&R.map), "r"(64 * p), "r"(R.head_first ? h : row), "r"(R.head_first ? row : h), "r"(page), "r"(kv),
+                                 "r"(full)
+                                 : "memory");
+            }
+        }
+    }
+}
+
+// fp8: raw tiles to f16 operand tiles, and the tokens' scales.
+template <int DP>
+__device__ __forceinline__ void rows_convert(const RowsParams &R, RowsShared &sh, const RowsWalk &k, const uint8_t *smem_ptr, uint32_t smem,
+                                             int tid)
+{
+    using C = RowsCfg<true, DP>;
+    const AttendParams &P = R.a;
+    constexpr int CPR = DP / 16, STEPS = CPR;
+    volatile uint32_t *abort_flag = &sh.abort_flag;
+    const int lane = tid & 31, warp = tid >> 5;
+    RowsAt a{k, k.t0, 0u, true};
+    float ks = 0.f, vs = 0.f;   // of this thread's token in the tile at `a`
+    auto look_up = [&]() {
+        ks = vs = 0.f;
+        const int tok = a.k.sp.first + a.t * kRowsTile + tid;
+        if (!a.more || tok < a.k.sp.lo || tok >= a.k.sp.hi || a.k.w.bad) return;
+        const int g = __ldg(P.seqs.page_table + (uint64_t)a.k.s * P.seqs.table_stride + P.cache.by_T.div((uint32_t)tok));
+        if ((uint32_t)g >= P.cache.num_pages) return;
+        ks = __ldg(P.cache.ks + (uint64_t)g * P.cache.s_page + a.k.h);
+        vs = __ldg(P.cache.vs + (uint64_t)g * P.cache.s_page + a.k.h);
+    };
+    look_up();
+    float vref = 0.f;
+    uint32_t part = 0xffffffffu, unit = 0;
+    bool ok = true;
+    for (uint32_t n = 0; a.more; ++n) {
+        if (a.part != part) {
+            part = a.part;
+            vref = 0.f;
+        }
+        float top = fabsf(vs);
+        if (!(top <= 3.402823466e38f)) top = 0.f;
+        top = __uint_as_float(__reduce_max_sync(0xffffffffu, __float_as_uint(top)));
+        if (lane == 0) sh.vtop[n & 1u][warp] = top;
+        ok = named_and(2, 128, ok);   // the converters give up together
+        if (!ok) return;
+        const float *v = sh.vtop[n & 1u];
+        top = fmaxf(fmaxf(v[0], v[1]), fmaxf(v[2], v[3]));
+        const float was = vref;
+        if (top > vref) vref = top;
+        const uint32_t slot = n % kRowsScaleSlots;
+        sh.ks[slot][tid] = ks;
+        sh.vs[slot][tid] = vref > 0.f ? vs * (C::kUp / vref) : 0.f;
+        if (tid == 0) {
+            sh.vref[slot] = vref;
+            sh.vdown[slot] = was == vref ? 1.f : was / vref;
+        }
+        __syncwarp();
+        if (lane == 0) mbar_arrive(smem_addr(&sh.scale_full[slot]));
+        at_next(P, a);
+        look_up();
+#pragma unroll 1
+        for (int kv = 0; kv < 2; ++kv, ++unit) {
+            const uint32_t rs = unit % kRowsRaw, st = unit % C::STAGES;
+            ok = ok && mbar_wait(smem_addr(&sh.raw_full[rs]), (unit / kRowsRaw) & 1u, abort_flag, R.error, 0x803u, R.wait_limit_ns);
+            if (unit >= C::STAGES)
+                ok = ok && mbar_wait(smem_addr(&sh.empty[st]), (unit / C::STAGES - 1u) & 1u, abort_flag, R.error, 0x804u, R.wait_limit_ns);
+            if (!ok) continue;
+            const uint8_t *src = smem_ptr + C::RAW_OFF + rs * C::RAW_BYTES;
+            const uint32_t dst = smem + C::KV_OFF + st * C::TILE_BYTES;
+#pragma unroll 4
+            for (int i = 0; i < STEPS; ++i) {
+                const uint32_t j = tid + 128u * i, r = j / CPR, c = j % CPR;
+                const uint4 x = *reinterpret_cast<const uint4 *>(src + 16u * j);
+                sts16(dst + tc_piece(r, 2u * c), e4m3_to_f16(x.x), e4m3_to_f16(x.x >> 16), e4m3_to_f16(x.y), e4m3_to_f16(x.y >> 16));
+                sts16(dst + tc_piece(r, 2u * c + 1u), e4m3_to_f16(x.z), e4m3_to_f16(x.z >> 16), e4m3_to_f16(x.w), e4m3_to_f16(x.w >> 16));
+            }
+            fence_async_smem();
+            mbar_arrive(smem_addr(&sh.full[st]));
+            mbar_arrive(smem_addr(&sh.raw_empty[rs]));
+        }
+    }
+}
+
+// K and V of the stretch's tiles, in the order K, V, K, V, row by row: any page size and row length.
 template <bool FP8, int DP>
 __device__ __forceinline__ void rows_load(const RowsParams &R, RowsShared &sh, RowsWalk k, uint32_t smem, int tid)
 {
@@ -302,21 +499,20 @@ __device__ __forceinline__ void rows_load(const RowsParams &R, RowsShared &sh, R
     auto announce = [&]() {
         copy_wait<0>();
         fence_async_smem();
-        for (; pending; --pending) mbar_arrive(smem_addr(&sh.full[(unit - pending) % kRowsStages]));
+        for (; pending; --pending) mbar_arrive(smem_addr(&sh.full[(unit - pending) % C::STAGES]));
     };
     auto wait_empty = [&](uint32_t u) -> bool {
-        if (u < kRowsStages) return true;
-        const uint32_t bar = smem_addr(&sh.empty[u % kRowsStages]), parity = (u / kRowsStages - 1u) & 1u;
+        if (u < C::STAGES) return true;
+        const uint32_t bar = smem_addr(&sh.empty[u % C::STAGES]), parity = (u / C::STAGES - 1u) & 1u;
         if (mbar_test_wait(bar, parity)) return true;
         if (!FP8) announce();   // the consumer may need what is in flight before it can free a stage
         return mbar_wait(bar, parity, abort_flag, R.error, 0x801u, R.wait_limit_ns);
     };
 
-    uint4 next[FP8 ? STEPS : 1];
     bool ok = true;
     do {
         float vref = 0.f;
-        if (tid == 0) sh.missing[(part_no + 4u) & 7u] = 0u;   // four parts ahead: nobody is there yet
+        if (tid == 0) sh.missing[(part_no + kRowsPartSlots / 2) % kRowsPartSlots] = 0u;   // nobody is there yet
         for (int t = k.t0; t < k.t1; ++t, ++tile_no) {
             const int tok = k.sp.first + t * kRowsTile + tid;
             long long at = -1;
@@ -344,10 +540,7 @@ __device__ __forceinline__ void rows_load(const RowsParams &R, RowsShared &sh, R
                 top = __uint_as_float(__reduce_max_sync(0xffffffffu, __float_as_uint(top)));
                 if (lane == 0) sh.vtop[tile_no & 1u][warp] = top;
             }
-            if (missing) {
-                sh.missing[part_no & 7u] = 1u;
-                if (P.seqs.status) P.seqs.status[k.s] = 2;  // GK_JOB_PAGE_TABLE
-            }
+            if (missing) mark_missing(P, sh, part_no, k.s);
             ok = named_and(2, 128, ok);   // the loaders give up together
             if (!ok) break;
             if (FP8) {
@@ -368,28 +561,21 @@ __device__ __forceinline__ void rows_load(const RowsParams &R, RowsShared &sh, R
 #pragma unroll
             for (int kv = 0; kv < 2; ++kv) {
                 const uint8_t *base = kv ? P.cache.v : P.cache.k;
+                ok = ok && wait_empty(unit);
+                if (!ok) continue;
+                const uint32_t dst = smem + C::KV_OFF + (unit % C::STAGES) * C::TILE_BYTES;
                 if (FP8) {
-#pragma unroll
+#pragma unroll 4
                     for (int i = 0; i < STEPS; ++i) {
                         const uint32_t j = tid + 128u * i, r = j / CPR, c = j % CPR;
                         const long long off = row_at[r];
-                        next[i] = make_uint4(0u, 0u, 0u, 0u);
-                        if (off >= 0 && c < pieces) next[i] = __ldg(reinterpret_cast<const uint4 *>(base + off + 16u * c));
-                    }
-                }
-                ok = ok && wait_empty(unit);
-                if (!ok) continue;
-                const uint32_t dst = smem + C::KV_OFF + (unit % kRowsStages) * C::TILE_BYTES;
-                if (FP8) {
-#pragma unroll
-                    for (int i = 0; i < STEPS; ++i) {
-                        const uint32_t j = tid + 128u * i, r = j / CPR, c = j % CPR;
-                        const uint4 x = next[i];
+                        uint4 x = make_uint4(0u, 0u, 0u, 0u);
+                        if (off >= 0 && c < pieces) x = __ldg(reinterpret_cast<const uint4 *>(base + off + 16u * c));
                         sts16(dst + tc_piece(r, 2u * c), e4m3_to_f16(x.x), e4m3_to_f16(x.x >> 16), e4m3_to_f16(x.y), e4m3_to_f16(x.y >> 16));
                         sts16(dst + tc_piece(r, 2u * c + 1u), e4m3_to_f16(x.z), e4m3_to_f16(x.z >> 16), e4m3_to_f16(x.w), e4m3_to_f16(x.w >> 16));
                     }
                     fence_async_smem();
-                    mbar_arrive(smem_addr(&sh.full[unit % kRowsStages]));
+                    mbar_arrive(smem_addr(&sh.full[unit % C::STAGES]));
                     ++unit;
                 } else {
 #pragma unroll
@@ -424,7 +610,7 @@ __device__ __forceinline__ void rows_mma(const RowsParams &R, RowsShared &sh, Ro
         return mbar_wait(smem_addr(bar), parity, abort_flag, R.error, where, R.wait_limit_ns);
     };
     auto add_values = [&](int i, uint32_t n, bool first) {  // O_i += P_i V
-        const uint32_t v = smem + C::KV_OFF + ((2u * n + 1u) % kRowsStages) * C::TILE_BYTES;
+        const uint32_t v = smem + C::KV_OFF + ((2u * n + 1u) % C::STAGES) * C::TILE_BYTES;
 #pragma unroll
         for (int s = 0; s < kRowsTile / 16; ++s)
             tc_mma_ts(tmem + 256u + i * 128u, tmem + i * 128u + 8u * s, tc_desc(v + s * 2048u, kRowsTile * 128u), kO, !first || s > 0);
@@ -435,8 +621,8 @@ __device__ __forceinline__ void rows_mma(const RowsParams &R, RowsShared &sh, Ro
         const int nt = k.t1 - k.t0;
         for (int t = 0; t <= nt; ++t) {
             const uint32_t n = tile_no + t, u = 2u * n;  // K's place among the loaded tiles
-            if (t < nt && !wait(&sh.full[u % kRowsStages], (u / kRowsStages) & 1u, 0x811u)) return;
-            if (t > 0 && !wait(&sh.full[(u - 1u) % kRowsStages], ((u - 1u) / kRowsStages) & 1u, 0x812u)) return;
+            if (t < nt && !wait(&sh.full[u % C::STAGES], (u / C::STAGES) & 1u, 0x811u)) return;
+            if (t > 0 && !wait(&sh.full[(u - 1u) % C::STAGES], ((u - 1u) / C::STAGES) & 1u, 0x812u)) return;
             for (int i = 0; i < act; ++i) {
                 if (t > 0) {
                     if (!wait(&sh.p_full[i], p_phase[i] & 1u, 0x813u)) return;
@@ -451,7 +637,7 @@ __device__ __forceinline__ void rows_mma(const RowsParams &R, RowsShared &sh, Ro
                         ++q_phase[i];
                         tc_fence_after();
                     }
-                    const uint32_t q = smem + C::Q_OFF + i * C::TILE_BYTES, kk = smem + C::KV_OFF + (u % kRowsStages) * C::TILE_BYTES;
+                    const uint32_t q = smem + C::Q_OFF + i * C::TILE_BYTES, kk = smem + C::KV_OFF + (u % C::STAGES) * C::TILE_BYTES;
 #pragma unroll
                     for (int s = 0; s < DP / 16; ++s) {
                         const uint32_t off = (s >> 2) * (kRowsTile * 128u) + (s & 3) * 32u;
@@ -460,8 +646,8 @@ __device__ __forceinline__ void rows_mma(const RowsParams &R, RowsShared &sh, Ro
                     tc_commit(smem_addr(&sh.s_full[i]));
                 }
             }
-            if (t > 0) tc_commit(smem_addr(&sh.empty[(u - 1u) % kRowsStages]));
-            if (t < nt) tc_commit(smem_addr(&sh.empty[u % kRowsStages]));
+            if (t > 0) tc_commit(smem_addr(&sh.empty[(u - 1u) % C::STAGES]));
+            if (t < nt) tc_commit(smem_addr(&sh.empty[u % C::STAGES]));
         }
         tile_no += nt;
     } while (walk_next(P, k));
@@ -511,10 +697,163 @@ __device__ __forceinline__ float rows_query(const RowsParams &R, const RowsWalk 
     return up;
 }
 
+// One warp: the parts of the stretch, each one ahead of the softmax warps.
+__device__ __forceinline__ void rows_parts(const RowsParams &R, RowsShared &sh, RowsWalk k, long long begin, long long ctas, int lane)
+{
+    const AttendParams &P = R.a;
+    volatile uint32_t *abort_flag = &sh.abort_flag;
+    long long place = begin;   // of the part's first tile in the line
+    bool more = true;
+    for (uint32_t n = 0;; ++n) {
+        if (lane == 0) {
+            RowsPart &w = sh.part[n & 1u];
+            w.end = !more || *abort_flag;
+            if (more) {
+                w.s = k.s;
+                w.q0 = k.w.q0;
+                w.at = k.w.at;
+                w.kv = k.w.kv;
+                w.blk = k.blk;
+                w.h = k.h;
+                w.rows = min(kRowsBlock, k.w.q_len * (int)P.G - k.blk * kRowsBlock);
+                w.first = k.sp.first + k.t0 * kRowsTile;
+                w.lo = k.sp.lo;
+                w.hi = k.sp.hi;
+                w.tiles = k.t1 - k.t0;
+                w.whole = k.t0 == 0 && k.t1 == k.sp.tiles;
+                w.starts = k.t0 == 0;
+                const long long item = place - k.t0;
+                w.c0 = (uint32_t)(((item + 1) * ctas - 1) / sh.total);
+                w.c1 = (uint32_t)(((item + k.sp.tiles) * ctas - 1) / sh.total);
+            }
+        }
+        __syncwarp();
+        named_sync(1, 288);
+        if (sh.part[n & 1u].end) return;
+        place += k.t1 - k.t0;
+        more = walk_next(P, k);
+    }
+}
+
+// Tokens that row `row` of a sequence attends to: [lo, hi).
+__device__ __forceinline__ void row_span(const AttendParams &P, int at, int kv, int row, int &lo, int &hi)
+{
+    const int pos = at + (int)P.by_G.div((uint32_t)row);
+    hi = P.causal ? min(max(0, pos + 1), kv) : kv;
+    lo = P.window ? (int)max(0ll, (long long)pos + 1 - (long long)P.window) : 0;
+}
+
+__device__ __forceinline__ __nv_bfloat16 *row_out(const AttendParams &P, int q0, int h, int row, uint64_t &lse_at)
+{
+    const uint32_t j = P.by_G.div((uint32_t)row);
+    const uint32_t head = (uint32_t)h * P.G + (uint32_t)(row - (int)(j * P.G));
+    lse_at = (uint64_t)(q0 + (int)j) * P.Hq + head;
+    return P.out + (uint64_t)(q0 + (int)j) * P.o_tok + (uint64_t)head * P.o_head;
+}
+
+__device__ __forceinline__ float max3(float a, float b, float c)
+{
+    float d;
+    asm("max.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(b), "f"(c));
+    return d;
+}
+
+// 0 * infinity must not reach rows that do not attend to a token, so infinities and NaN of a V tile become 0 here;
+// bad_lo and bad_hi tell the end of the part where to look for those that some row does attend to.
+template <bool FP8, int DP>
+__device__ __noinline__ void clean_values(RowsShared &sh, uint8_t *v, int tok0, int lo, int hi, int r)
+{
+    bool found = false;
+    for (int c = r; c < RowsCfg<FP8, DP>::TILE_BYTES / 16; c += 128) {
+        uint32_t *w = reinterpret_cast<uint32_t *>(v + 16 * c);
+        const uint4 x = *reinterpret_cast<const uint4 *>(w);
+        const uint32_t y[4] = {x.x, x.y, x.z, x.w};
+        constexpr uint32_t E = FP8 ? 0x7c00u : 0x7f80u;
+        bool hit = false;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) hit |= (y[e] & E) == E || (y[e] & (E << 16)) == (E << 16);
+        if (hit) {
+            found = true;
+            const int tok = tok0 + (c & (8 * kRowsTile - 1)) / 8;
+            if (tok >= lo && tok < hi) {   // others are nobody's: the rest of a page, or never loaded
+                atomicMin(&sh.bad_lo, tok);
+                atomicMax(&sh.bad_hi, tok + 1);
+                __threadfence_block();
+            }
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                uint32_t z = y[e];
+                if ((z & E) == E) z &= 0xffff0000u;
+                if ((z & (E << 16)) == (E << 16)) z &= 0xffffu;
+                w[e] = z;
+            }
+        }
+    }
+    if (found) fence_async_smem();
+}
+
+// Infinities and NaN that the products left out, added to 32 outputs of a row that attends to [lo, hi) of them.
+template <bool FP8>
+__device__ __noinline__ void add_not_finite(const AttendParams &P, uint32_t s, int h, int lo, int hi, int d0, float *o)
+{
+    for (int t = lo; t < hi; ++t) {
+        const uint32_t page = P.cache.by_T.div((uint32_t)t);
+        const int g = __ldg(P.seqs.page_table + (uint64_t)s * P.seqs.table_stride + page);
+        if ((uint32_t)g >= P.cache.num_pages) continue;
+        const uint8_t *v = P.cache.v + (uint64_t)g * P.cache.page + (uint64_t)((uint32_t)t - page * P.cache.T) * P.cache.tok +
+                           (uint64_t)h * P.cache.head;
+        for (int e = 0; e < 32 && d0 + e < (int)P.cache.D; ++e) {
+            const float y = FP8 ? __half2float(__half(__nv_cvt_fp8_to_halfraw(v[d0 + e], __NV_E4M3)))
+                                : __bfloat162float(reinterpret_cast<const __nv_bfloat16 *>(v)[d0 + e]);
+            if (!(fabsf(y) <= 3.402823466e38f)) o[e * kRowsBlock] += y;
+        }
+    }
+}
+
+// One row's parts in the order of the line: 32 outputs from d on, and the row's maximum and sum.
+template <int DP>
+__device__ __forceinline__ void join_row(const float *parts, uint32_t c0, uint32_t c1, int prow, int d, float (&v)[32], float &m, float &l)
+{
+    constexpr size_t PF = (size_t)kRowsBlock * (DP + 2);
+    m = -INFINITY;
+    for (uint32_t c = c0; c <= c1; ++c)
+        m = fmaxf(m, __ldcg(parts + (2u * c + (c == c0 ? 1u : 0u)) * PF + kRowsBlock * DP + prow));
+    const float ref = m == -INFINITY ? 0.f : m;
+    l = 0.f;
+#pragma unroll
+    for (int e = 0; e < 32; ++e) v[e] = 0.f;
+#pragma unroll 2
+    for (uint32_t c = c0; c <= c1; ++c) {
+        const float *p = parts + (2u * c + (c == c0 ? 1u : 0u)) * PF;
+        const float f = fast_exp2(__ldcg(p + kRowsBlock * DP + prow) - ref);
+        l += f * __ldcg(p + kRowsBlock * (DP + 1) + prow);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            const float4 y = __ldcg(reinterpret_cast<const float4 *>(p + (size_t)((d / 4 + e) * kRowsBlock + prow) * 4));
+            v[4 * e] += f * y.x;
+            v[4 * e + 1] += f * y.y;
+            v[4 * e + 2] += f * y.z;
+            v[4 * e + 3] += f * y.w;
+        }
+    }
+}
+
+__device__ __forceinline__ void store_row(const AttendParams &P, __nv_bfloat16 *out, int d, const float (&v)[32], float f)
+{
+#pragma unroll
+    for (int e = 0; e < 32; e += 8)
+        if (d + e < (int)P.cache.D)
+            *reinterpret_cast<uint4 *>(out + d + e) =
+                make_uint4(bf16x2(v[e] * f, v[e + 1] * f), bf16x2(v[e + 2] * f, v[e + 3] * f), bf16x2(v[e + 4] * f, v[e + 5] * f),
+                           bf16x2(v[e + 6] * f, v[e + 7] * f));
+}
+
+__device__ __forceinline__ float lse_of(float m, float l) { return l == 0.f ? -INFINITY : m * 0.69314718055994531f + logf(l); }
+
 // Softmax and output of one tile of 128 rows: one thread per row.
 template <bool FP8, int DP>
-__device__ __forceinline__ void rows_softmax(const RowsParams &R, RowsShared &sh, RowsWalk k, long long begin, long long ctas,
-                                             uint8_t *smem_ptr, uint32_t smem, uint32_t tmem, int i, int tid)
+__device__ __forceinline__ void rows_softmax(const RowsParams &R, RowsShared &sh, uint8_t *smem_ptr, uint32_t smem, uint32_t tmem, int i,
+                                             int tid)
 {
     using C = RowsCfg<FP8, DP>;
     const AttendParams &P = R.a;
@@ -522,111 +861,95 @@ __device__ __forceinline__ void rows_softmax(const RowsParams &R, RowsShared &sh
     const int lane = tid & 31, r = tid & 127;
     const uint32_t my = tmem + ((uint32_t)(r & 96) << 16);   // this warp's lanes
     const uint32_t s_at = my + i * 128u, o_at = my + 256u + i * 128u;
-    uint32_t tile_no = 0, part_no = 0, s_phase = 0, o_phase = 0;
-    long long place = begin;   // of the current part's first tile in the line
-    bool ok = true;
-    for (;;) {
-        const int rows = min(kRowsBlock, k.w.q_len * (int)P.G - k.blk * kRowsBlock);
-        const int row = k.blk * kRowsBlock + i * kRowsTile + r;   // row of the sequence: token * G + head of the group
-        const bool active = i * kRowsTile < rows;
-        const bool live = i * kRowsTile + r < rows;
-        const int nt = k.t1 - k.t0;
-        const bool whole = k.t0 == 0 && k.t1 == k.sp.tiles;
-        const long long item = place - k.t0;
-        float m = -INFINITY, l = 0.f, vref = 1.f, mul = R.scale_log2;
-        int lo = 0, hi = 0;
-        // tokens that every live row of this tile attends to: [all_lo, all_hi)
-        int all_lo = 0, all_hi = 0;
-        if (active && (P.causal || P.window)) {
-            const int p0 = k.w.at + (int)P.by_G.div((uint32_t)(k.blk * kRowsBlock + i * kRowsTile));
-            const int p1 = k.w.at + (int)P.by_G.div((uint32_t)(k.blk * kRowsBlock + min(rows, (i + 1) * kRowsTile) - 1));
-            all_hi = P.causal ? min(max(0, p0 + 1), k.w.kv) : k.w.kv;
-            all_lo = P.window ? (int)max(0ll, (long long)p1 + 1 - (long long)P.window) : 0;
-        } else {
-            all_hi = k.w.kv;
-        }
+    const int prow = i * kRowsTile + r;
+    uint32_t n = 0;                       // tiles so far, of both
+    uint32_t s_phase = 0, o_phase = 0;
+    for (uint32_t part_no = 0;; ++part_no) {
+        named_sync(1, 288);
+        const RowsPart &w = sh.part[part_no & 1u];
+        if (w.end) return;
+        const int nt = w.tiles;
+        const bool active = i * kRowsTile < w.rows;
+        const bool live = prow < w.rows;
         if (tid == 0) {
             sh.bad_lo = 0x7fffffff;
             sh.bad_hi = 0;
-            sh.stop = *abort_flag;
         }
-        named_sync(1, 256);
-        if (sh.stop) return;   // both tiles' threads together
+        named_sync(3, 256);
+        float m = -INFINITY, l = 0.f, vref = 1.f;
+        int lo = 0, hi = 0;
+        bool ok = true;
         if (active) {
-            if (live) {
-                const int pos = k.w.at + (int)P.by_G.div((uint32_t)row);
-                hi = P.causal ? min(max(0, pos + 1), k.w.kv) : k.w.kv;
-                lo = P.window ? (int)max(0ll, (long long)pos + 1 - (long long)P.window) : 0;
+            if (live) row_span(P, w.at, w.kv, w.blk * kRowsBlock + prow, lo, hi);
+            float mul = R.scale_log2;
+            {
+                RowsWalk k;
+                k.w.q0 = w.q0;
+                k.h = w.h;
+                mul *= rows_query<FP8, DP>(R, k, smem + C::Q_OFF + i * C::TILE_BYTES, r, w.blk * kRowsBlock + prow, live);
             }
-            mul *= rows_query<FP8, DP>(R, k, smem + C::Q_OFF + i * C::TILE_BYTES, r, row, live);
             fence_async_smem();
             __syncwarp();
             if (lane == 0) mbar_arrive(smem_addr(&sh.q_full[i]));
-            float2 sum = make_float2(0.f, 0.f);
-            for (int t = 0; t < nt; ++t) {
-                const uint32_t n = tile_no + t;
-                const int tok0 = k.sp.first + (k.t0 + t) * kRowsTile;
+            // tokens that every live row of this tile attends to
+            int all_lo, all_hi, x0, x1;
+            row_span(P, w.at, w.kv, w.blk * kRowsBlock + i * kRowsTile, x0, all_hi);
+            row_span(P, w.at, w.kv, w.blk * kRowsBlock + min(w.rows, (i + 1) * kRowsTile) - 1, all_lo, x1);
+            float2 sum[2] = {};
+            int tok0 = w.first;
+            for (int t = 0; t < nt; ++t, tok0 += kRowsTile) {
                 ok = mbar_wait(smem_addr(&sh.s_full[i]), s_phase & 1u, abort_flag, R.error, 0x821u, R.wait_limit_ns);
                 ++s_phase;
-                if (!__all_sync(0xffffffffu, ok)) {
-                    ok = false;
-                    break;
-                }
+                ok = __all_sync(0xffffffffu, ok);
+                if (!ok) break;
                 tc_fence_after();
-                uint32_t raw[128];
-#pragma unroll
-                for (int c = 0; c < 4; ++c) tc_ld32(raw + 32 * c, s_at + 32u * c);
+                float2 s[64];
+                uint32_t *raw = reinterpret_cast<uint32_t *>(s);
+                tc_ld32(raw, s_at);
+                tc_ld32(raw + 32, s_at + 32u);
                 tc_wait_ld();
-                float2 *s = reinterpret_cast<float2 *>(raw);
-                const uint32_t slot = n % kRowsScaleSlots;
+                tc_ld32(raw + 64, s_at + 64u);
+                tc_ld32(raw + 96, s_at + 96u);
+                const uint32_t slot = (n + t) % kRowsScaleSlots;
                 float down_v = 1.f;
-                if (FP8) {
-                    mbar_wait(smem_addr(&sh.scale_full[slot]), (n / kRowsScaleSlots) & 1u, abort_flag, R.error, 0x822u, R.wait_limit_ns);
-                    const float2 *ks = reinterpret_cast<const float2 *>(sh.ks[slot]);
+                const bool edge = tok0 < all_lo || tok0 + kRowsTile > all_hi;   // the same for all 128 threads
+                if (FP8)
+                    mbar_wait(smem_addr(&sh.scale_full[slot]), ((n + t) / kRowsScaleSlots) & 1u, abort_flag, R.error, 0x822u,
+                              R.wait_limit_ns);
+                float top4[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+                auto half_done = [&](int c0) {
+                    if (FP8) {
+                        const float4 *ks = reinterpret_cast<const float4 *>(sh.ks[slot]);
 #pragma unroll
-                    for (int c = 0; c < 64; ++c) s[c] = mul2(s[c], ks[c]);
+                        for (int c = c0 / 2; c < c0 / 2 + 16; ++c) {
+                            const float4 f = ks[c];
+                            s[2 * c] = mul2(s[2 * c], make_float2(f.x, f.y));
+                            s[2 * c + 1] = mul2(s[2 * c + 1], make_float2(f.z, f.w));
+                        }
+                    }
+                    if (edge) {
+#pragma unroll
+                        for (int c = c0; c < c0 + 32; ++c) {
+                            if (tok0 + 2 * c < lo || tok0 + 2 * c >= hi) s[c].x = -INFINITY;
+                            if (tok0 + 2 * c + 1 < lo || tok0 + 2 * c + 1 >= hi) s[c].y = -INFINITY;
+                        }
+                    }
+#pragma unroll
+                    for (int c = c0; c < c0 + 32; ++c) top4[c & 3] = max3(top4[c & 3], s[c].x, s[c].y);
+                };
+                half_done(0);
+                tc_wait_ld();
+                half_done(32);
+                if (edge) {
+                    const uint32_t vu = 2u * (n + t) + 1u;
+                    mbar_wait(smem_addr(&sh.full[vu % C::STAGES]), (vu / C::STAGES) & 1u, abort_flag, R.error, 0x823u, R.wait_limit_ns);
+                    clean_values<FP8, DP>(sh, smem_ptr + C::KV_OFF + (vu % C::STAGES) * C::TILE_BYTES, tok0, w.lo, w.hi, r);
+                }
+                if (FP8) {
                     vref = sh.vref[slot];
                     down_v = sh.vdown[slot];
                 }
-                if (__any_sync(0xffffffffu, tok0 < lo || tok0 + kRowsTile > hi)) {
-#pragma unroll
-                    for (int c = 0; c < 128; ++c)
-                        if (tok0 + c < lo || tok0 + c >= hi) raw[c] = 0xff800000u;
-                }
-                if (tok0 < all_lo || min(tok0 + kRowsTile, k.sp.hi) > all_hi) {
-                    // 0 * infinity must not reach rows that do not attend to a token: such V are set to 0 here and added
-                    // to the rows that do in the end
-                    const uint32_t vu = 2u * n + 1u;
-                    mbar_wait(smem_addr(&sh.full[vu % kRowsStages]), (vu / kRowsStages) & 1u, abort_flag, R.error, 0x823u, R.wait_limit_ns);
-                    uint8_t *v = smem_ptr + C::KV_OFF + (vu % kRowsStages) * C::TILE_BYTES;
-                    bool found = false;
-                    for (int c = r; c < C::TILE_BYTES / 16; c += 128) {
-                        uint32_t *w = reinterpret_cast<uint32_t *>(v + 16 * c);
-                        const uint4 x = *reinterpret_cast<const uint4 *>(w);
-                        const uint32_t y[4] = {x.x, x.y, x.z, x.w};
-                        constexpr uint32_t E = FP8 ? 0x7c00u : 0x7f80u;
-                        bool hit = false;
-#pragma unroll
-                        for (int e = 0; e < 4; ++e) hit |= (y[e] & E) == E || (y[e] & (E << 16)) == (E << 16);
-                        if (hit) {
-                            found = true;
-                            atomicMin(&sh.bad_lo, tok0);
-                            atomicMax(&sh.bad_hi, tok0 + kRowsTile);
-                            __threadfence_block();
-#pragma unroll
-                            for (int e = 0; e < 4; ++e) {
-                                uint32_t z = y[e];
-                                if ((z & E) == E) z &= 0xffff0000u;
-                                if ((z & (E << 16)) == (E << 16)) z &= 0xffffu;
-                                w[e] = z;
-                            }
-                        }
-                    }
-                    if (found) fence_async_smem();
-                }
-                float top = -INFINITY;
-#pragma unroll
-                for (int c = 0; c < 128; c += 2) top = fmaxf(top, fmaxf(s[c / 2].x, s[c / 2].y));
+                const float top = fmaxf(fmaxf(top4[0], top4[1]), fmaxf(top4[2], top4[3]));
                 const float x = top * mul;
                 if (t == 0) {
                     m = top == -INFINITY ? -INFINITY : x;
@@ -634,17 +957,17 @@ __device__ __forceinline__ void rows_softmax(const RowsParams &R, RowsShared &sh
                     const float nm = top == -INFINITY ? m : fmaxf(m, x);
                     const float f = nm == m ? 1.f : fast_exp2(m - nm);
                     m = nm;
-                    sum.x *= f;
-                    sum.y *= f;
+                    sum[0] = mul2(sum[0], make_float2(f, f));
+                    sum[1] = mul2(sum[1], make_float2(f, f));
                     const float g = f * down_v;
-                    uint32_t o[32];
-#pragma unroll
-                    for (int c = 0; c < DP / 32; ++c) {
-                        tc_ld32(o, o_at + 32u * c);
+                    uint32_t o[16];
+#pragma unroll 1
+                    for (int c = 0; c < DP / 16; ++c) {
+                        tc_ld16(o, o_at + 16u * c);
                         tc_wait_ld();
 #pragma unroll
-                        for (int e = 0; e < 32; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * g);
-                        tc_st32(o_at + 32u * c, o);
+                        for (int e = 0; e < 16; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * g);
+                        tc_st16(o_at + 16u * c, o);
                     }
                 }
                 const float ref = m == -INFINITY ? 0.f : -m;
@@ -657,12 +980,12 @@ __device__ __forceinline__ void rows_softmax(const RowsParams &R, RowsShared &sh
                         float2 e = fma2(s[16 * c4 + c], mul_2, ref_2);
                         e.x = fast_exp2(e.x);
                         e.y = fast_exp2(e.y);
-                        sum = add2(sum, e);
+                        sum[c & 1] = add2(sum[c & 1], e);
                         if (FP8) {
                             const float2 v = reinterpret_cast<const float2 *>(sh.vs[slot])[16 * c4 + c];
-                            const float2 w = mul2(e, v);
+                            const float2 y = mul2(e, v);
                             // a masked token stays 0 whatever its scale is
-                            pk[c] = f16x2(e.x == 0.f ? 0.f : w.x, e.y == 0.f ? 0.f : w.y);
+                            pk[c] = f16x2(e.x == 0.f ? 0.f : y.x, e.y == 0.f ? 0.f : y.y);
                         } else {
                             pk[c] = bf16x2(e.x, e.y);
                         }
@@ -674,68 +997,51 @@ __device__ __forceinline__ void rows_softmax(const RowsParams &R, RowsShared &sh
                 __syncwarp();
                 if (lane == 0) mbar_arrive(smem_addr(&sh.p_full[i]));
             }
-            l = sum.x + sum.y;
+            l = (sum[0].x + sum[0].y) + (sum[1].x + sum[1].y);
+            if (ok) {
+                ok = mbar_wait(smem_addr(&sh.o_full[i]), o_phase & 1u, abort_flag, R.error, 0x824u, R.wait_limit_ns);
+                ++o_phase;
+                ok = __all_sync(0xffffffffu, ok);
+            }
         }
-        float *part = P.parts + (uint64_t)(2u * blockIdx.x + (k.t0 > 0 ? 0u : 1u)) * C::PART_FLOATS;
-        const int prow = i * kRowsTile + r;
-        if (active && ok) {
-            ok = mbar_wait(smem_addr(&sh.o_full[i]), o_phase & 1u, abort_flag, R.error, 0x824u, R.wait_limit_ns);
-            ++o_phase;
-            ok = __all_sync(0xffffffffu, ok);
-        }
-        named_sync(1, 256);   // both tiles are through: bad_lo and bad_hi are final
-        const uint32_t j = P.by_G.div((uint32_t)(live ? row : 0));
-        const uint32_t head = (uint32_t)k.h * P.G + (uint32_t)((live ? row : 0) - (int)(j * P.G));
-        __nv_bfloat16 *out = P.out + (uint64_t)(k.w.q0 + j) * P.o_tok + (uint64_t)head * P.o_head;
+        named_sync(3, 256);   // both tiles are through: bad_lo and bad_hi are final
+        uint64_t lse_at;
+        __nv_bfloat16 *out = row_out(P, w.q0, w.h, w.blk * kRowsBlock + (live ? prow : 0), lse_at);
+        float *part = P.parts + (uint64_t)(2u * blockIdx.x + (w.starts ? 1u : 0u)) * C::PART_FLOATS;
         if (active && ok) {
             tc_fence_after();
-            if (sh.missing[part_no & 7u]) l = __int_as_float(0x7fc00000);
-            const int bad_lo = max(sh.bad_lo, lo), bad_hi = min(sh.bad_hi, hi);
+            if (sh.missing[part_no % kRowsPartSlots]) l = __int_as_float(0x7fc00000);
             const float back = FP8 ? vref * (1.f / C::kUp) : 1.f;
-            const float inv = !whole ? back : l == 0.f ? 0.f : back / l;
+            const float inv = !w.whole ? back : l == 0.f ? 0.f : back / l;
+            const bool bad = sh.bad_lo < sh.bad_hi;
 #pragma unroll 1
             for (int c = 0; c < DP / 32; ++c) {
-                uint32_t o[32];
+                float o[32];
                 __syncwarp();
-                tc_ld32(o, o_at + 32u * c);
+                tc_ld32(reinterpret_cast<uint32_t *>(o), o_at + 32u * c);
                 tc_wait_ld();
-                if (live) {
-                    for (int t = bad_lo; t < bad_hi; ++t) {   // infinities and NaN that the products left out
-                        const uint32_t page = P.cache.by_T.div((uint32_t)t);
-                        const int g = __ldg(P.seqs.page_table + (uint64_t)k.s * P.seqs.table_stride + page);
-                        if ((uint32_t)g >= P.cache.num_pages) continue;
-                        const uint8_t *v = P.cache.v + (uint64_t)g * P.cache.page + (uint64_t)((uint32_t)t - page * P.cache.T) * P.cache.tok +
-                                           (uint64_t)k.h * P.cache.head;
+                if (bad) {
+                    // by way of the query tile, which nobody needs any more: dimension-major, so that threads do not meet
+                    float *room = reinterpret_cast<float *>(smem_ptr + C::Q_OFF) + prow;
 #pragma unroll
-                        for (int e = 0; e < 32; ++e) {
-                            const int d = 32 * c + e;
-                            if (d >= (int)P.cache.D) continue;
-                            const float y = FP8 ? __half2float(__half(__nv_cvt_fp8_to_halfraw(v[d], __NV_E4M3)))
-                                                : __bfloat162float(reinterpret_cast<const __nv_bfloat16 *>(v)[d]);
-                            if (!(fabsf(y) <= 3.402823466e38f)) o[e] = __float_as_uint(__uint_as_float(o[e]) + y);
-                        }
-                    }
+                    for (int e = 0; e < 32; ++e) room[e * kRowsBlock] = o[e];
+                    if (live) add_not_finite<FP8>(P, w.s, w.h, max(sh.bad_lo, lo), min(sh.bad_hi, hi), 32 * c, room);
 #pragma unroll
-                    for (int e = 0; e < 32; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * inv);
-                    if (whole) {
+                    for (int e = 0; e < 32; ++e) o[e] = room[e * kRowsBlock];
+                }
+                if (!live) continue;
+                if (w.whole) {
+                    store_row(P, out, 32 * c, o, inv);
+                } else {
 #pragma unroll
-                        for (int e = 0; e < 32; e += 8)
-                            if (32 * c + e < (int)P.cache.D) {
-                                const float *f = reinterpret_cast<const float *>(o) + e;
-                                *reinterpret_cast<uint4 *>(out + 32 * c + e) =
-                                    make_uint4(bf16x2(f[0], f[1]), bf16x2(f[2], f[3]), bf16x2(f[4], f[5]), bf16x2(f[6], f[7]));
-                            }
-                    } else {
-#pragma unroll
-                        for (int e = 0; e < 32; e += 4)
-                            *reinterpret_cast<uint4 *>(part + (size_t)((32 * c + e) / 4 * kRowsBlock + prow) * 4) =
-                                make_uint4(o[e], o[e + 1], o[e + 2], o[e + 3]);
-                    }
+                    for (int e = 0; e < 32; e += 4)
+                        *reinterpret_cast<float4 *>(part + (size_t)((32 * c + e) / 4 * kRowsBlock + prow) * 4) =
+                            make_float4(o[e] * inv, o[e + 1] * inv, o[e + 2] * inv, o[e + 3] * inv);
                 }
             }
             if (live) {
-                if (whole) {
-                    if (P.lse) P.lse[(uint64_t)(k.w.q0 + j) * P.Hq + head] = l == 0.f ? -INFINITY : m * 0.69314718055994531f + logf(l);
+                if (w.whole) {
+                    if (P.lse) P.lse[lse_at] = lse_of(m, l);
                 } else {
                     part[kRowsBlock * DP + prow] = m;
                     part[kRowsBlock * (DP + 1) + prow] = l;
@@ -743,61 +1049,58 @@ __device__ __forceinline__ void rows_softmax(const RowsParams &R, RowsShared &sh
             }
             tc_fence_before();
         }
-        if (!whole) {
-            // the CTAs that share the block: those whose stretches hold its first and its last tile
-            const uint32_t c0 = (uint32_t)(((item + 1) * ctas - 1) / sh.total);
-            const uint32_t c1 = (uint32_t)(((item + k.sp.tiles) * ctas - 1) / sh.total);
-            __threadfence();
-            named_sync(1, 256);
-            if (tid == 0) {
-                const uint32_t seen = atomicAdd(P.counters + c0, 1u);
-                sh.last = seen == c1 - c0;
-                if (seen == c1 - c0) P.counters[c0] = 0u;  // ready for the next call
-            }
-            named_sync(1, 256);
-            if (sh.last && live) {
+        if (!w.whole) {
+            const uint32_t more = w.c1 - w.c0;
+            if (R.join && more >= kRowsHere) {
+                if (tid == 0 && w.starts) R.join[blockIdx.x] = RowsJoin{more + 1u, w.s, w.blk, w.h};
+            } else {
                 __threadfence();
-                float jm = -INFINITY;
-                for (uint32_t c = c0; c <= c1; ++c)
-                    jm = fmaxf(jm, __ldcg(P.parts + (uint64_t)(2u * c + (c == c0 ? 1u : 0u)) * C::PART_FLOATS + kRowsBlock * DP + prow));
-                const float ref = jm == -INFINITY ? 0.f : jm;
-                float jl = 0.f;
-#pragma unroll 1
-                for (int d = 0; d < (int)P.cache.D; d += 16) {
-                    float4 v[4] = {};
-                    jl = 0.f;
-                    for (uint32_t c = c0; c <= c1; ++c) {
-                        const float *p = P.parts + (uint64_t)(2u * c + (c == c0 ? 1u : 0u)) * C::PART_FLOATS;
-                        const float f = fast_exp2(__ldcg(p + kRowsBlock * DP + prow) - ref);
-                        jl += f * __ldcg(p + kRowsBlock * (DP + 1) + prow);
-#pragma unroll
-                        for (int e = 0; e < 4; ++e) {
-                            const float4 y = __ldcg(reinterpret_cast<const float4 *>(p + (size_t)((d / 4 + e) * kRowsBlock + prow) * 4));
-                            v[e].x += f * y.x;
-                            v[e].y += f * y.y;
-                            v[e].z += f * y.z;
-                            v[e].w += f * y.w;
-                        }
-                    }
-                    const float inv = jl == 0.f ? 0.f : 1.f / jl;
-#pragma unroll
-                    for (int e = 0; e < 4; e += 2)
-                        *reinterpret_cast<uint4 *>(out + d + 4 * e) =
-                            make_uint4(bf16x2(v[e].x * inv, v[e].y * inv), bf16x2(v[e].z * inv, v[e].w * inv),
-                                       bf16x2(v[e + 1].x * inv, v[e + 1].y * inv), bf16x2(v[e + 1].z * inv, v[e + 1].w * inv));
+                named_sync(3, 256);
+                if (tid == 0) {
+                    const uint32_t seen = atomicAdd(P.counters + w.c0, 1u);
+                    sh.last = seen == more;
+                    if (seen == more) P.counters[w.c0] = 0u;  // ready for the next call
                 }
-                if (P.lse) P.lse[(uint64_t)(k.w.q0 + j) * P.Hq + head] = jl == 0.f ? -INFINITY : jm * 0.69314718055994531f + logf(jl);
+                named_sync(3, 256);
+                if (sh.last && live) {
+                    __threadfence();
+                    float jm, jl;
+#pragma unroll 1
+                    for (int d = 0; d < (int)P.cache.D; d += 32) {
+                        float v[32];
+                        join_row<DP>(P.parts, w.c0, w.c1, prow, d, v, jm, jl);
+                        store_row(P, out, d, v, jl == 0.f ? 0.f : 1.f / jl);
+                    }
+                    if (P.lse) P.lse[lse_at] = lse_of(jm, jl);
+                }
             }
         }
-        tile_no += nt;
-        place += nt;
-        ++part_no;
-        if (!walk_next(P, k)) return;
+        n += nt;
     }
 }
 
+// Blocks that many CTAs share: 32 rows and 32 outputs of each a warp.
+template <int DP>
+__global__ void __launch_bounds__(128) join_rows_kernel(const __grid_constant__ RowsParams R)
+{
+    const AttendParams &P = R.a;
+    asm volatile("griddepcontrol.wait;" ::: "memory");
+    const RowsJoin j = R.join[blockIdx.x];
+    const int d = 32 * (threadIdx.x >> 5), prow = (int)blockIdx.y * 32 + (threadIdx.x & 31);
+    if (j.parts == 0 || d >= (int)P.cache.D) return;
+    const RowsSeq w = rows_seq(P, j.s);
+    const int row = j.blk * kRowsBlock + prow;
+    if (row >= w.q_len * (int)P.G) return;
+    float v[32], m, l;
+    join_row<DP>(P.parts, blockIdx.x, blockIdx.x + j.parts - 1u, prow, d, v, m, l);
+    uint64_t lse_at;
+    __nv_bfloat16 *out = row_out(P, w.q0, j.h, row, lse_at);
+    store_row(P, out, d, v, l == 0.f ? 0.f : 1.f / l);
+    if (P.lse && d == 0) P.lse[lse_at] = lse_of(m, l);
+}
+
 template <bool FP8, int DP>
-__global__ void __launch_bounds__(kRowsThreads, 1) attend_rows_kernel(const RowsParams R)
+__global__ void __launch_bounds__(kRowsThreads, 1) attend_rows_kernel(const __grid_constant__ RowsParams R)
 {
     using C = RowsCfg<FP8, DP>;
     const AttendParams &P = R.a;
@@ -806,6 +1109,8 @@ __global__ void __launch_bounds__(kRowsThreads, 1) attend_rows_kernel(const Rows
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
     uint8_t *smem_ptr = smem_raw + ((1024u - (smem_addr(smem_raw) & 1023u)) & 1023u);
     const uint32_t smem = smem_addr(smem_ptr);
+    if (R.join && tid == 0) R.join[blockIdx.x].parts = 0u;   // tid 0 also enters a block there
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
 
     // the length of the line of tiles
     long long total = 0;
@@ -878,9 +1183,13 @@ __global__ void __launch_bounds__(kRowsThreads, 1) attend_rows_kernel(const Rows
         }
     }
     if (tid == 0) {
-        for (int i = 0; i < kRowsStages; ++i) {
-            mbar_init(smem_addr(&sh.full[i]), 128);
+        for (int i = 0; i < C::STAGES; ++i) {
+            mbar_init(smem_addr(&sh.full[i]), !FP8 && R.tma ? 1 : 128);
             mbar_init(smem_addr(&sh.empty[i]), 1);
+        }
+        for (int i = 0; i < kRowsRaw; ++i) {
+            mbar_init(smem_addr(&sh.raw_full[i]), 1);
+            mbar_init(smem_addr(&sh.raw_empty[i]), 128);
         }
         for (int i = 0; i < 2; ++i) {
             mbar_init(smem_addr(&sh.q_full[i]), 4);
@@ -891,7 +1200,7 @@ __global__ void __launch_bounds__(kRowsThreads, 1) attend_rows_kernel(const Rows
         for (int i = 0; i < kRowsScaleSlots; ++i) mbar_init(smem_addr(&sh.scale_full[i]), 4);
         mbar_init(smem_addr(&sh.drained), 1);
         sh.abort_flag = 0u;
-        for (int i = 0; i < 8; ++i) sh.missing[i] = 0u;
+        for (int i = 0; i < kRowsPartSlots; ++i) sh.missing[i] = 0u;
         sh.total = total;
         fence_mbar_init();
     }
@@ -915,11 +1224,12 @@ __global__ void __launch_bounds__(kRowsThreads, 1) attend_rows_kernel(const Rows
     k.t1 = min(k.sp.tiles, k.t0 + k.left);
 
     if (warp < 8) {
-        asm volatile("setmaxnreg.inc.sync.aligned.u32 184;");
-        rows_softmax<FP8, DP>(R, sh, k, begin, ctas, smem_ptr, smem, tmem, warp >> 2, tid);
+        asm volatile("setmaxnreg.inc.sync.aligned.u32 200;");
+        rows_softmax<FP8, DP>(R, sh, smem_ptr, smem, tmem, warp >> 2, tid);
     } else if (warp < 12) {
-        asm volatile("setmaxnreg.dec.sync.aligned.u32 96;");
-        rows_load<FP8, DP>(R, sh, k, smem, tid - 256);
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 64;");
+        if (!R.tma) rows_load<FP8, DP>(R, sh, k, smem, tid - 256);
+        else if (FP8) rows_convert<DP>(R, sh, k, smem_ptr, smem, tid - 256);
     } else {
         asm volatile("setmaxnreg.dec.sync.aligned.u32 48;");
         if (tid == 12 * 32) {
@@ -927,6 +1237,10 @@ __global__ void __launch_bounds__(kRowsThreads, 1) attend_rows_kernel(const Rows
             // whatever has been issued ends before the tensor memory is given back
             tc_commit(smem_addr(&sh.drained));
             mbar_drain(smem_addr(&sh.drained), 0u, 4ull * R.wait_limit_ns);
+        } else if (warp == 13 && R.tma) {
+            rows_fetch<FP8, DP>(R, sh, k, smem, lane);
+        } else if (warp == 14) {
+            rows_parts(R, sh, k, begin, ctas, lane);
         }
         __syncwarp();
     }

@@ -98,8 +98,9 @@ int check_rope(gk_ctx *c, const gk_rope *r, RopeDev *out)
     return GK_OK;
 }
 
-// Workspace of gk_attention: join counters, then two partial results per CTA of the largest grid.
+// Workspace of gk_attention: join counters, blocks for the join kernel, two partial results per CTA of the largest grid.
 constexpr size_t kAttnCounterBytes = 4096;
+constexpr size_t kAttnJoinBytes = 16384;
 constexpr int kAttnMaxCtas = 1024;
 
 int ensure_attention(gk_ctx *c)
@@ -108,7 +109,8 @@ int ensure_attention(gk_ctx *c)
     const size_t part = (size_t)(kAttendRows * 256 + 2 * kAttendRows) * 4;
     const size_t few = 2 * (size_t)kAttnMaxCtas * part;
     const size_t many = 2 * (size_t)c->sm_count * RowsCfg<false, 128>::PART_FLOATS * 4;
-    const size_t bytes = kAttnCounterBytes + (few > many ? few : many);
+    static_assert(sizeof(RowsJoin) == 16, "");
+    const size_t bytes = kAttnCounterBytes + kAttnJoinBytes + (few > many ? few : many);
     if (cudaMalloc(&c->d_attn, bytes) != cudaSuccess) {
         cudaGetLastError();
         c->d_attn = nullptr;
@@ -144,6 +146,42 @@ int launch_attend(gk_ctx *c, const AttendParams &P, cudaStream_t st)
     return GK_OK;
 }
 
+typedef CUresult (*EncodeTiled)(CUtensorMap *, CUtensorMapDataType, cuuint32_t, void *, const cuuint64_t *, const cuuint64_t *,
+                                const cuuint32_t *, const cuuint32_t *, CUtensorMapInterleave, CUtensorMapSwizzle,
+                                CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+
+// The tensor map of a layer's K and V, if its pages tile 128 tokens and its rows are whole copies; P.tma says so.
+void make_map(const gk_ctx *c, const gk_cache *k, RowsParams &P)
+{
+    static const EncodeTiled encode = [] {
+        void *f = nullptr;
+        cudaDriverEntryPointQueryResult r;
+        if (cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &f, 12000, cudaEnableDefault, &r) != cudaSuccess ||
+            r != cudaDriverEntryPointSuccess) {
+            cudaGetLastError();
+            f = nullptr;
+        }
+        return (EncodeTiled)f;
+    }();
+    const LayerDev &l = P.a.cache;
+    const bool fp8 = c->geom.dtype == GK_FP8_E4M3;
+    P.tma = 0;
+    if (!encode || (l.D != 64 && l.D != 128)) return;
+    if (l.T % 8 != 0 || (l.T < 128 ? 128 % l.T != 0 : l.T % 128 != 0)) return;
+    const uint64_t far = 1ull << 39;
+    if (l.page >= far || k->kv_stride >= far || l.page == 0 || k->kv_stride == 0) return;
+    P.head_first = c->gd.head_major ? 0u : 1u;
+    P.page_rows = l.T < 128 ? l.T : 128u;
+    P.per_tile = 128u / P.page_rows;
+    const cuuint64_t dims[5] = {l.D, P.head_first ? l.H : l.T, P.head_first ? l.T : l.H, l.num_pages, 2};
+    const cuuint64_t strides[4] = {P.head_first ? l.head : l.tok, P.head_first ? l.tok : l.head, l.page, k->kv_stride};
+    const cuuint32_t box[5] = {fp8 ? l.D : 64u, P.head_first ? 1u : P.page_rows, P.head_first ? P.page_rows : 1u, 1u, 1u};
+    const cuuint32_t ones[5] = {1, 1, 1, 1, 1};
+    P.tma = encode(&P.map, fp8 ? CU_TENSOR_MAP_DATA_TYPE_UINT8 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 5, l.k, dims, strides, box, ones,
+                   CU_TENSOR_MAP_INTERLEAVE_NONE, fp8 ? CU_TENSOR_MAP_SWIZZLE_NONE : CU_TENSOR_MAP_SWIZZLE_128B,
+                   CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
 template <bool FP8, int DP>
 int launch_rows(gk_ctx *c, const RowsParams &P, cudaStream_t st)
 {
@@ -160,6 +198,19 @@ int launch_rows(gk_ctx *c, const RowsParams &P, cudaStream_t st)
     attend_rows_kernel<FP8, DP><<<c->sm_count, kRowsThreads, C::SMEM, st>>>(P);
     GK_CUDA(c, cudaGetLastError());
     c->stats.kernels_launched++;
+    if (P.join) {
+        cudaLaunchConfig_t cfg{};
+        cfg.gridDim = dim3(c->sm_count, kRowsBlock / 32);
+        cfg.blockDim = dim3(DP);
+        cfg.stream = st;
+        cudaLaunchAttribute at{};
+        at.id = cudaLaunchAttributeProgrammaticStreamSerialization;
+        at.val.programmaticStreamSerializationAllowed = 1;
+        cfg.attrs = &at;
+        cfg.numAttrs = 1;
+        GK_CUDA(c, cudaLaunchKernelEx(&cfg, join_rows_kernel<DP>, P));
+        c->stats.kernels_launched++;
+    }
     return GK_OK;
 }
 
@@ -248,7 +299,7 @@ int gk_attention(gk_ctx *c, const gk_cache *cache, uint32_t layer, const gk_batc
     P.causal = (flags & GK_ATTN_FULL) ? 0u : 1u;
     P.window = window;
     P.counters = (uint32_t *)c->d_attn;
-    P.parts = (float *)(c->d_attn + kAttnCounterBytes);
+    P.parts = (float *)(c->d_attn + kAttnCounterBytes + kAttnJoinBytes);
     const cudaStream_t st = (cudaStream_t)stream;
     const uint32_t D = c->geom.head_dim;
     const uint32_t max_q = batch->q_start ? (batch->max_q_len ? batch->max_q_len : batch->n_tokens) : 1u;
@@ -259,6 +310,11 @@ int gk_attention(gk_ctx *c, const gk_cache *cache, uint32_t layer, const gk_batc
         R.q_sign = scale == 0.f ? 0.f : scale < 0.f ? -1.f : 1.f;
         R.error = c->d_error;
         R.wait_limit_ns = c->wait_limit_ns;
+        make_map(c, cache, R);
+        // Few blocks mean many CTAs to a block, whose parts one CTA would be long to join; with two blocks per CTA and more
+        // that happens in lopsided batches only.
+        const uint64_t blocks = ((uint64_t)batch->n_tokens * P.G / kRowsBlock + batch->n_seqs) * c->geom.kv_heads;
+        if (blocks < 2ull * c->sm_count) R.join = (RowsJoin *)(c->d_attn + kAttnCounterBytes);
         if (c->geom.dtype == GK_FP8_E4M3) return D <= 64 ? launch_rows<true, 64>(c, R, st) : launch_rows<true, 128>(c, R, st);
         return D <= 64 ? launch_rows<false, 64>(c, R, st) : launch_rows<false, 128>(c, R, st);
     }
