@@ -18,8 +18,8 @@
 // ring of its own, from which warps 8-11 convert to f16.  Pages that do not tile 128 tokens (or whose rows are not 64 or
 // 128 values) are loaded by warps 8-11 alone, row by row.
 //
-// Work is dealt out as in attend_kernel: the token tiles of all blocks lie in one line, every CTA takes an equal
-// stretch, parts of a block meet in the workspace.
+// Work is dealt out as in attend_kernel: the token tiles of all blocks lie in one line (with some units more for
+// every block), every CTA takes an equal stretch, parts of a block meet in the workspace.
 #pragma once
 
 #include <cuda.h>  // CUtensorMap
@@ -34,6 +34,8 @@ constexpr int kRowsBlock = 2 * kRowsTile;
 constexpr int kRowsThreads = 512;
 constexpr int kRowsRaw = 3;                  // fp8 tiles in flight
 constexpr int kRowsScaleSlots = 4;
+constexpr int kRowsGroup = 8;                // tokens that share a scale wherever tensor copies are used
+constexpr int kRowsParts = 4;                // parts that the softmax warps may know of at a time
 constexpr int kRowsPartSlots = 16;           // more than the parts between the first and the last role
 
 // A block that more than kRowsHere CTAs share: joined by a kernel of its own.
@@ -84,15 +86,19 @@ __device__ __forceinline__ void fence_async_smem() { asm volatile("fence.proxy.a
 
 __device__ __forceinline__ void tc_commit(uint32_t bar)
 {
-    asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(bar) : "memory");
+    asm volatile("{ .reg .pred e; elect.sync _|e, 0xffffffff;\n"
+                 "@e tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0]; }" ::"r"(bar) : "memory");
 }
 
 // shared-memory operand descriptor: 128-byte swizzle, groups of 8 rows 1024 bytes apart; `lead` is the distance
 // between 64-value pieces of an operand whose contiguous dimension is not the summed one (V)
-__device__ __forceinline__ uint64_t tc_desc(uint32_t addr, uint32_t lead)
+__device__ __forceinline__ uint32_t tc_desc_low(uint32_t addr, uint32_t lead) { return ((addr & 0x3ffffu) >> 4) | ((lead >> 4) << 16); }
+__device__ __forceinline__ uint64_t tc_desc(uint32_t low)
 {
-    return (uint64_t)((addr & 0x3ffffu) >> 4) | ((uint64_t)(lead >> 4) << 16) | ((uint64_t)(1024u >> 4) << 32) |
-           (1ull << 46) | (2ull << 61);
+    constexpr uint32_t high = (1024u >> 4) | (1u << 14) | (2u << 29);
+    uint64_t d;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(d) : "r"(low), "r"(high));
+    return d;
 }
 
 // M = 128, fp32 accumulators; f16 or bf16 operands; b_mn: B's contiguous dimension is N
@@ -102,15 +108,18 @@ __host__ __device__ constexpr uint32_t tc_idesc(bool f16, int n, bool b_mn)
            ((128u >> 4) << 24);
 }
 
+// The whole warp comes here, so that operands stay in uniform registers; one elected lane issues.
 __device__ __forceinline__ void tc_mma_ss(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, bool add)
 {
-    asm volatile("{ .reg .pred p; setp.ne.u32 p, %4, 0; tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p; }" ::"r"(d),
+    asm volatile("{ .reg .pred p, e; setp.ne.u32 p, %4, 0; elect.sync _|e, 0xffffffff;\n"
+                 "@e tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p; }" ::"r"(d),
                  "l"(a), "l"(b), "r"(idesc), "r"((uint32_t)add)
                  : "memory");
 }
 __device__ __forceinline__ void tc_mma_ts(uint32_t d, uint32_t a, uint64_t b, uint32_t idesc, bool add)
 {
-    asm volatile("{ .reg .pred p; setp.ne.u32 p, %4, 0; tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p; }" ::"r"(d),
+    asm volatile("{ .reg .pred p, e; setp.ne.u32 p, %4, 0; elect.sync _|e, 0xffffffff;\n"
+                 "@e tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p; }" ::"r"(d),
                  "r"(a), "l"(b), "r"(idesc), "r"((uint32_t)add)
                  : "memory");
 }
@@ -181,13 +190,17 @@ __device__ __forceinline__ RowsSpan rows_span(const AttendParams &P, const RowsS
     return r;
 }
 
-// Tiles of a sequence for one key head, for each lane its own sequence; the warp helps with long ones.
+// A block counts for its tiles and kRowsCost more: loading the queries, starting and draining the pipeline and writing the
+// outputs take about as long as that many tiles.  The extra units come first.
+constexpr int kRowsCost = 3;
+
+// Units of a sequence for one key head, for each lane its own sequence; the warp helps with long ones.
 __device__ __forceinline__ long long rows_tiles(const AttendParams &P, const RowsSeq &w, int lane)
 {
     long long n = 0;
     const bool own = w.blocks <= 4;
     if (own)
-        for (int b = 0; b < w.blocks; ++b) n += rows_span(P, w, b).tiles;
+        for (int b = 0; b < w.blocks; ++b) n += rows_span(P, w, b).tiles + kRowsCost;
     uint32_t rest = __ballot_sync(0xffffffffu, !own);
     while (rest) {
         const int src = __ffs(rest) - 1;
@@ -199,7 +212,7 @@ __device__ __forceinline__ long long rows_tiles(const AttendParams &P, const Row
         o.blocks = __shfl_sync(0xffffffffu, w.blocks, src);
         o.bad = __shfl_sync(0xffffffffu, (int)w.bad, src) != 0;
         long long m = 0;
-        for (int b = lane; b < o.blocks; b += 32) m += rows_span(P, o, b).tiles;
+        for (int b = lane; b < o.blocks; b += 32) m += rows_span(P, o, b).tiles + kRowsCost;
 #pragma unroll
         for (int k = 16; k; k >>= 1) m += __shfl_xor_sync(0xffffffffu, m, k);
         if (lane == src) n = m;
@@ -214,13 +227,13 @@ struct RowsWalk {
     RowsSpan sp;
     int blk, h;
     int t0, t1;   // tiles of the current part
-    int left;     // tiles of the stretch from t0 on
+    long long reach;  // units from the block's first tile to the end of the stretch
 };
 
 __device__ __forceinline__ bool walk_next(const AttendParams &P, RowsWalk &k)
 {
-    k.left -= k.t1 - k.t0;
-    if (k.left <= 0) return false;
+    k.reach -= k.sp.tiles + kRowsCost;
+    if (k.reach <= 0) return false;
     k.t0 = 0;
     if (++k.h == (int)P.cache.H) {
         k.h = 0;
@@ -233,7 +246,7 @@ __device__ __forceinline__ bool walk_next(const AttendParams &P, RowsWalk &k)
         }
         k.sp = rows_span(P, k.w, k.blk);
     }
-    k.t1 = min(k.sp.tiles, k.left);
+    k.t1 = (int)min((long long)k.sp.tiles, k.reach);
     return true;
 }
 
@@ -247,22 +260,25 @@ struct RowsPart {
     bool whole, starts;    // the part is the whole block; it holds the block's first tile
     uint32_t c0, c1;       // CTAs that share the block
     bool end;
+    int bad_lo, bad_hi;    // tokens among which V holds infinities or NaN that not every row may see
 };
 
 struct RowsShared {
-    unsigned long long full[4], empty[4], raw_full[kRowsRaw], raw_empty[kRowsRaw], q_full[2], s_full[2], p_full[2], o_full[2], scale_full[kRowsScaleSlots];
+    unsigned long long full[4], empty[4], raw_full[kRowsRaw], raw_empty[kRowsRaw], q_full[2], s_full[2], p_half[2], p_full[2], o_full[2],
+        scale_full[kRowsScaleSlots], part_full[kRowsParts], part_empty[kRowsParts];
     unsigned long long drained;
     long long total, begin, before;
     uint32_t seq;
-    int blk, h, tile;
-    uint32_t tmem, abort_flag, beat, last;
-    RowsPart part[2];
-    int bad_lo, bad_hi;  // tokens among which V holds infinities or NaN that not every row may see
+    int blk, h, unit;
+    uint32_t tmem, abort_flag, last[2];
+    RowsPart part[kRowsParts];
     long long warp_sum[16];
     long long row_at[2][kRowsTile];  // byte offset of each token of a tile, or -1
     uint32_t missing[kRowsPartSlots];             // a page that the table should have held is missing: by part, in turn
     float ks[kRowsScaleSlots][kRowsTile], vs[kRowsScaleSlots][kRowsTile];
+    float ks8[kRowsScaleSlots][kRowsTile / kRowsGroup], vs8[kRowsScaleSlots][kRowsTile / kRowsGroup];
     float vref[kRowsScaleSlots], vdown[kRowsScaleSlots], vtop[2][4];
+    uint32_t plain[kRowsScaleSlots], odd[2][4];   // scales are equal within groups, positive and finite
 };
 
 __device__ __forceinline__ void named_sync(int id, int threads)
@@ -440,7 +456,11 @@ __device__ __forceinline__ void rows_convert(const RowsParams &R, RowsShared &sh
         float top = fabsf(vs);
         if (!(top <= 3.402823466e38f)) top = 0.f;
         top = __uint_as_float(__reduce_max_sync(0xffffffffu, __float_as_uint(top)));
-        if (lane == 0) sh.vtop[n & 1u][warp] = top;
+        const bool odd = __any_sync(0xffffffffu, !(ks >= 0.f && ks <= 3.402823466e38f && vs >= 0.f && vs <= 3.402823466e38f));
+        if (lane == 0) {
+            sh.vtop[n & 1u][warp] = top;
+            sh.odd[n & 1u][warp] = odd;
+        }
         ok = named_and(2, 128, ok);   // the converters give up together
         if (!ok) return;
         const float *v = sh.vtop[n & 1u];
@@ -448,11 +468,24 @@ __device__ __forceinline__ void rows_convert(const RowsParams &R, RowsShared &sh
         const float was = vref;
         if (top > vref) vref = top;
         const uint32_t slot = n % kRowsScaleSlots;
+        const float vw = vref > 0.f ? vs * (C::kUp / vref) : 0.f;
         sh.ks[slot][tid] = ks;
-        sh.vs[slot][tid] = vref > 0.f ? vs * (C::kUp / vref) : 0.f;
+        sh.vs[slot][tid] = vw;
+        // the first token of a group may lie before the window or the last behind the end: the largest is the group's
+        float kg = fmaxf(ks, __shfl_xor_sync(0xffffffffu, ks, 1)), vg = fmaxf(vw, __shfl_xor_sync(0xffffffffu, vw, 1));
+#pragma unroll
+        for (int o = 2; o < kRowsGroup; o <<= 1) {
+            kg = fmaxf(kg, __shfl_xor_sync(0xffffffffu, kg, o));
+            vg = fmaxf(vg, __shfl_xor_sync(0xffffffffu, vg, o));
+        }
+        if (lane % kRowsGroup == 0) {
+            sh.ks8[slot][tid / kRowsGroup] = kg;
+            sh.vs8[slot][tid / kRowsGroup] = vg;
+        }
         if (tid == 0) {
             sh.vref[slot] = vref;
             sh.vdown[slot] = was == vref ? 1.f : was / vref;
+            sh.plain[slot] = !(sh.odd[n & 1u][0] | sh.odd[n & 1u][1] | sh.odd[n & 1u][2] | sh.odd[n & 1u][3]);
         }
         __syncwarp();
         if (lane == 0) mbar_arrive(smem_addr(&sh.scale_full[slot]));
@@ -553,6 +586,7 @@ __device__ __forceinline__ void rows_load(const RowsParams &R, RowsShared &sh, R
                 if (tid == 0) {
                     sh.vref[slot] = vref;
                     sh.vdown[slot] = was == vref ? 1.f : was / vref;
+                    sh.plain[slot] = 0u;
                 }
                 __syncwarp();
                 if (lane == 0) mbar_arrive(smem_addr(&sh.scale_full[slot]));
@@ -596,7 +630,7 @@ __device__ __forceinline__ void rows_load(const RowsParams &R, RowsShared &sh, R
     announce();
 }
 
-// All MMAs, by one thread.
+// All MMAs, by one warp.
 template <bool FP8, int DP>
 __device__ __forceinline__ void rows_mma(const RowsParams &R, RowsShared &sh, RowsWalk k, uint32_t smem, uint32_t tmem)
 {
@@ -607,13 +641,14 @@ __device__ __forceinline__ void rows_mma(const RowsParams &R, RowsShared &sh, Ro
     uint32_t tile_no = 0;
     uint32_t p_phase[2] = {0, 0}, q_phase[2] = {0, 0};
     auto wait = [&](unsigned long long *bar, uint32_t parity, uint32_t where) {
-        return mbar_wait(smem_addr(bar), parity, abort_flag, R.error, where, R.wait_limit_ns);
+        return __all_sync(0xffffffffu, mbar_wait(smem_addr(bar), parity, abort_flag, R.error, where, R.wait_limit_ns)) != 0;
     };
-    auto add_values = [&](int i, uint32_t n, bool first) {  // O_i += P_i V
-        const uint32_t v = smem + C::KV_OFF + ((2u * n + 1u) % C::STAGES) * C::TILE_BYTES;
+    auto add_values = [&](int i, uint32_t n, bool first, int half) {  // O_i += P_i V, half of the tile's tokens
+        const uint32_t v = tc_desc_low(smem + C::KV_OFF + ((2u * n + 1u) % C::STAGES) * C::TILE_BYTES, kRowsTile * 128u) + half * (4u * 2048u >> 4);
+        const uint32_t p = tmem + i * 128u + half * 32u;
 #pragma unroll
-        for (int s = 0; s < kRowsTile / 16; ++s)
-            tc_mma_ts(tmem + 256u + i * 128u, tmem + i * 128u + 8u * s, tc_desc(v + s * 2048u, kRowsTile * 128u), kO, !first || s > 0);
+        for (int s = 0; s < kRowsTile / 32; ++s)
+            tc_mma_ts(tmem + 256u + i * 128u, p + 8u * s, tc_desc(v + s * (2048u >> 4)), kO, !first || s > 0);
     };
     do {
         const int rows = min(kRowsBlock, k.w.q_len * (int)P.G - k.blk * kRowsBlock);
@@ -625,10 +660,13 @@ __device__ __forceinline__ void rows_mma(const RowsParams &R, RowsShared &sh, Ro
             if (t > 0 && !wait(&sh.full[(u - 1u) % C::STAGES], ((u - 1u) / C::STAGES) & 1u, 0x812u)) return;
             for (int i = 0; i < act; ++i) {
                 if (t > 0) {
-                    if (!wait(&sh.p_full[i], p_phase[i] & 1u, 0x813u)) return;
+                    if (!wait(&sh.p_half[i], p_phase[i] & 1u, 0x813u)) return;
+                    tc_fence_after();
+                    add_values(i, n - 1u, t == 1, 0);
+                    if (!wait(&sh.p_full[i], p_phase[i] & 1u, 0x815u)) return;
                     ++p_phase[i];
                     tc_fence_after();
-                    add_values(i, n - 1u, t == 1);
+                    add_values(i, n - 1u, false, 1);
                     if (t == nt) tc_commit(smem_addr(&sh.o_full[i]));
                 }
                 if (t < nt) {
@@ -637,11 +675,12 @@ __device__ __forceinline__ void rows_mma(const RowsParams &R, RowsShared &sh, Ro
                         ++q_phase[i];
                         tc_fence_after();
                     }
-                    const uint32_t q = smem + C::Q_OFF + i * C::TILE_BYTES, kk = smem + C::KV_OFF + (u % C::STAGES) * C::TILE_BYTES;
+                    const uint32_t q = tc_desc_low(smem + C::Q_OFF + i * C::TILE_BYTES, 16u);
+                    const uint32_t kk = tc_desc_low(smem + C::KV_OFF + (u % C::STAGES) * C::TILE_BYTES, 16u);
 #pragma unroll
                     for (int s = 0; s < DP / 16; ++s) {
-                        const uint32_t off = (s >> 2) * (kRowsTile * 128u) + (s & 3) * 32u;
-                        tc_mma_ss(tmem + i * 128u, tc_desc(q + off, 16u), tc_desc(kk + off, 16u), kS, s > 0);
+                        const uint32_t off = ((s >> 2) * (kRowsTile * 128u) + (s & 3) * 32u) >> 4;
+                        tc_mma_ss(tmem + i * 128u, tc_desc(q + off), tc_desc(kk + off), kS, s > 0);
                     }
                     tc_commit(smem_addr(&sh.s_full[i]));
                 }
@@ -655,25 +694,29 @@ __device__ __forceinline__ void rows_mma(const RowsParams &R, RowsShared &sh, Ro
 
 // This thread's query row into shared memory, as f16 (fp8 caches, divided by a power of two that is returned) or bf16.
 template <bool FP8, int DP>
-__device__ __forceinline__ float rows_query(const RowsParams &R, const RowsWalk &k, uint32_t dst, int r, int row, bool live)
+__device__ __forceinline__ float rows_query(const RowsParams &R, const RowsPart &w, uint32_t dst, int r, int row, bool live)
 {
     const AttendParams &P = R.a;
     float up = 1.f;
     const uint32_t j = P.by_G.div((uint32_t)(live ? row : 0));
-    const uint32_t head = (uint32_t)k.h * P.G + (uint32_t)((live ? row : 0) - (int)(j * P.G));
-    const __nv_bfloat16 *p = P.q + (uint64_t)(k.w.q0 + j) * P.q_tok + (uint64_t)head * P.q_head;
+    const uint32_t head = (uint32_t)w.h * P.G + (uint32_t)((live ? row : 0) - (int)(j * P.G));
+    const __nv_bfloat16 *p = P.q + (uint64_t)(w.q0 + (int)j) * P.q_tok + (uint64_t)head * P.q_head;
     const uint32_t pieces = P.cache.D / 8u;
     float down = R.q_sign;
+    uint4 x[DP / 8];
+#pragma unroll
+    for (uint32_t c = 0; c < DP / 8; ++c) {
+        x[c] = make_uint4(0u, 0u, 0u, 0u);
+        if (live && c < pieces) x[c] = __ldg(reinterpret_cast<const uint4 *>(p) + c);
+    }
     if (FP8) {
         uint32_t top = 0;
-#pragma unroll 4
+#pragma unroll
         for (uint32_t c = 0; c < DP / 8; ++c) {
-            uint4 x = make_uint4(0u, 0u, 0u, 0u);
-            if (live && c < pieces) x = __ldg(reinterpret_cast<const uint4 *>(p) + c);
-            const uint32_t w[4] = {x.x, x.y, x.z, x.w};
+            const uint32_t y[4] = {x[c].x, x[c].y, x[c].z, x[c].w};
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
-                const uint32_t a = w[e] & 0x7fffu, b = (w[e] >> 16) & 0x7fffu;
+                const uint32_t a = y[e] & 0x7fffu, b = (y[e] >> 16) & 0x7fffu;
                 if (a < 0x7f80u) top = max(top, a);
                 if (b < 0x7f80u) top = max(top, b);
             }
@@ -682,55 +725,56 @@ __device__ __forceinline__ float rows_query(const RowsParams &R, const RowsWalk 
         down *= __uint_as_float((uint32_t)(127 - ex) << 23);
         up = __uint_as_float((uint32_t)(127 + ex) << 23);
     }
-#pragma unroll 4
-    for (uint32_t c = 0; c < DP / 8; ++c) {
-        uint4 x = make_uint4(0u, 0u, 0u, 0u);
-        if (live && c < pieces) x = __ldg(reinterpret_cast<const uint4 *>(p) + c);
-        uint32_t w[4] = {x.x, x.y, x.z, x.w};
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-            const float a = __uint_as_float(w[e] << 16) * down, b = __uint_as_float(w[e] & 0xffff0000u) * down;
-            w[e] = FP8 ? f16x2(a, b) : bf16x2(a, b);
+    for (uint32_t c = 0; c < DP / 8; ++c) {
+        uint32_t y[4] = {x[c].x, x[c].y, x[c].z, x[c].w};
+        if (FP8 || R.q_sign != 1.f) {
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const float a = __uint_as_float(y[e] << 16) * down, b = __uint_as_float(y[e] & 0xffff0000u) * down;
+                y[e] = FP8 ? f16x2(a, b) : bf16x2(a, b);
+            }
         }
-        sts16(dst + tc_piece(r, c), w[0], w[1], w[2], w[3]);
+        sts16(dst + tc_piece(r, c), y[0], y[1], y[2], y[3]);
     }
     return up;
 }
 
-// One warp: the parts of the stretch, each one ahead of the softmax warps.
-__device__ __forceinline__ void rows_parts(const RowsParams &R, RowsShared &sh, RowsWalk k, long long begin, long long ctas, int lane)
+// One thread: the parts of the stretch, ahead of the softmax warps.
+__device__ __forceinline__ void rows_parts(const RowsParams &R, RowsShared &sh, RowsWalk k, long long end, long long ctas)
 {
     const AttendParams &P = R.a;
     volatile uint32_t *abort_flag = &sh.abort_flag;
-    long long place = begin;   // of the part's first tile in the line
     bool more = true;
     for (uint32_t n = 0;; ++n) {
-        if (lane == 0) {
-            RowsPart &w = sh.part[n & 1u];
-            w.end = !more || *abort_flag;
-            if (more) {
-                w.s = k.s;
-                w.q0 = k.w.q0;
-                w.at = k.w.at;
-                w.kv = k.w.kv;
-                w.blk = k.blk;
-                w.h = k.h;
-                w.rows = min(kRowsBlock, k.w.q_len * (int)P.G - k.blk * kRowsBlock);
-                w.first = k.sp.first + k.t0 * kRowsTile;
-                w.lo = k.sp.lo;
-                w.hi = k.sp.hi;
-                w.tiles = k.t1 - k.t0;
-                w.whole = k.t0 == 0 && k.t1 == k.sp.tiles;
-                w.starts = k.t0 == 0;
-                const long long item = place - k.t0;
-                w.c0 = (uint32_t)(((item + 1) * ctas - 1) / sh.total);
-                w.c1 = (uint32_t)(((item + k.sp.tiles) * ctas - 1) / sh.total);
-            }
+        const uint32_t slot = n % kRowsParts;
+        if (n >= kRowsParts && !mbar_wait(smem_addr(&sh.part_empty[slot]), (n / kRowsParts - 1u) & 1u, abort_flag, R.error, 0x831u,
+                                          R.wait_limit_ns))
+            return;
+        RowsPart &w = sh.part[slot];
+        w.end = !more;
+        if (more) {
+            w.s = k.s;
+            w.q0 = k.w.q0;
+            w.at = k.w.at;
+            w.kv = k.w.kv;
+            w.blk = k.blk;
+            w.h = k.h;
+            w.rows = min(kRowsBlock, k.w.q_len * (int)P.G - k.blk * kRowsBlock);
+            w.first = k.sp.first + k.t0 * kRowsTile;
+            w.lo = k.sp.lo;
+            w.hi = k.sp.hi;
+            w.tiles = k.t1 - k.t0;
+            w.whole = k.t0 == 0 && k.t1 == k.sp.tiles;
+            w.starts = k.t0 == 0;
+            const long long first = end - k.reach;   // the unit of the block's first tile
+            w.c0 = (uint32_t)(((first + 1) * ctas - 1) / sh.total);
+            w.c1 = (uint32_t)(((first + k.sp.tiles) * ctas - 1) / sh.total);
+            w.bad_lo = 0x7fffffff;
+            w.bad_hi = 0;
         }
-        __syncwarp();
-        named_sync(1, 288);
-        if (sh.part[n & 1u].end) return;
-        place += k.t1 - k.t0;
+        mbar_arrive(smem_addr(&sh.part_full[slot]));
+        if (!more) return;
         more = walk_next(P, k);
     }
 }
@@ -761,7 +805,7 @@ __device__ __forceinline__ float max3(float a, float b, float c)
 // 0 * infinity must not reach rows that do not attend to a token, so infinities and NaN of a V tile become 0 here;
 // bad_lo and bad_hi tell the end of the part where to look for those that some row does attend to.
 template <bool FP8, int DP>
-__device__ __noinline__ void clean_values(RowsShared &sh, uint8_t *v, int tok0, int lo, int hi, int r)
+__device__ __noinline__ void clean_values(RowsPart &part, uint8_t *v, int tok0, int lo, int hi, int r)
 {
     bool found = false;
     for (int c = r; c < RowsCfg<FP8, DP>::TILE_BYTES / 16; c += 128) {
@@ -776,8 +820,8 @@ __device__ __noinline__ void clean_values(RowsShared &sh, uint8_t *v, int tok0, 
             found = true;
             const int tok = tok0 + (c & (8 * kRowsTile - 1)) / 8;
             if (tok >= lo && tok < hi) {   // others are nobody's: the rest of a page, or never loaded
-                atomicMin(&sh.bad_lo, tok);
-                atomicMax(&sh.bad_hi, tok + 1);
+                atomicMin(&part.bad_lo, tok);
+                atomicMax(&part.bad_hi, tok + 1);
                 __threadfence_block();
             }
 #pragma unroll
@@ -794,18 +838,21 @@ __device__ __noinline__ void clean_values(RowsShared &sh, uint8_t *v, int tok0, 
 
 // Infinities and NaN that the products left out, added to 32 outputs of a row that attends to [lo, hi) of them.
 template <bool FP8>
-__device__ __noinline__ void add_not_finite(const AttendParams &P, uint32_t s, int h, int lo, int hi, int d0, float *o)
+__device__ __forceinline__ void add_not_finite(const AttendParams &P, const RowsPart &w, int lo, int hi, int d0, float (&o)[32])
 {
+#pragma unroll 1
     for (int t = lo; t < hi; ++t) {
         const uint32_t page = P.cache.by_T.div((uint32_t)t);
-        const int g = __ldg(P.seqs.page_table + (uint64_t)s * P.seqs.table_stride + page);
+        const int g = __ldg(P.seqs.page_table + (uint64_t)w.s * P.seqs.table_stride + page);
         if ((uint32_t)g >= P.cache.num_pages) continue;
         const uint8_t *v = P.cache.v + (uint64_t)g * P.cache.page + (uint64_t)((uint32_t)t - page * P.cache.T) * P.cache.tok +
-                           (uint64_t)h * P.cache.head;
-        for (int e = 0; e < 32 && d0 + e < (int)P.cache.D; ++e) {
+                           (uint64_t)w.h * P.cache.head;
+#pragma unroll
+        for (int e = 0; e < 32; ++e) {
+            if (d0 + e >= (int)P.cache.D) continue;
             const float y = FP8 ? __half2float(__half(__nv_cvt_fp8_to_halfraw(v[d0 + e], __NV_E4M3)))
                                 : __bfloat162float(reinterpret_cast<const __nv_bfloat16 *>(v)[d0 + e]);
-            if (!(fabsf(y) <= 3.402823466e38f)) o[e * kRowsBlock] += y;
+            if (!(fabsf(y) <= 3.402823466e38f)) o[e] += y;
         }
     }
 }
@@ -864,33 +911,36 @@ __device__ __forceinline__ void rows_softmax(const RowsParams &R, RowsShared &sh
     const int prow = i * kRowsTile + r;
     uint32_t n = 0;                       // tiles so far, of both
     uint32_t s_phase = 0, o_phase = 0;
-    for (uint32_t part_no = 0;; ++part_no) {
-        named_sync(1, 288);
-        const RowsPart &w = sh.part[part_no & 1u];
-        if (w.end) return;
+    // the next part, known to all four warps or to none, and its queries
+    auto next_part = [&](uint32_t no) -> bool {
+        const bool ok = mbar_wait(smem_addr(&sh.part_full[no % kRowsParts]), (no / kRowsParts) & 1u, abort_flag, R.error, 0x826u,
+                                  R.wait_limit_ns);
+        return named_and(3 + i, 128, ok) && !sh.part[no % kRowsParts].end;
+    };
+    auto queries = [&](const RowsPart &w) -> float {
+        float mul = R.scale_log2;
+        if (i * kRowsTile < w.rows) {
+            mul *= rows_query<FP8, DP>(R, w, smem + C::Q_OFF + i * C::TILE_BYTES, r, w.blk * kRowsBlock + prow, prow < w.rows);
+            fence_async_smem();
+            __syncwarp();
+            if (lane == 0) mbar_arrive(smem_addr(&sh.q_full[i]));
+        }
+        return mul;
+    };
+    if (!next_part(0)) return;
+    float next_mul = queries(sh.part[0]);
+    bool more = true;
+    for (uint32_t part_no = 0; more; ++part_no) {
+        RowsPart &w = sh.part[part_no % kRowsParts];
         const int nt = w.tiles;
         const bool active = i * kRowsTile < w.rows;
         const bool live = prow < w.rows;
-        if (tid == 0) {
-            sh.bad_lo = 0x7fffffff;
-            sh.bad_hi = 0;
-        }
-        named_sync(3, 256);
+        const float mul = next_mul;
         float m = -INFINITY, l = 0.f, vref = 1.f;
         int lo = 0, hi = 0;
         bool ok = true;
         if (active) {
             if (live) row_span(P, w.at, w.kv, w.blk * kRowsBlock + prow, lo, hi);
-            float mul = R.scale_log2;
-            {
-                RowsWalk k;
-                k.w.q0 = w.q0;
-                k.h = w.h;
-                mul *= rows_query<FP8, DP>(R, k, smem + C::Q_OFF + i * C::TILE_BYTES, r, w.blk * kRowsBlock + prow, live);
-            }
-            fence_async_smem();
-            __syncwarp();
-            if (lane == 0) mbar_arrive(smem_addr(&sh.q_full[i]));
             // tokens that every live row of this tile attends to
             int all_lo, all_hi, x0, x1;
             row_span(P, w.at, w.kv, w.blk * kRowsBlock + i * kRowsTile, x0, all_hi);
@@ -912,20 +962,21 @@ __device__ __forceinline__ void rows_softmax(const RowsParams &R, RowsShared &sh
                 tc_ld32(raw + 96, s_at + 96u);
                 const uint32_t slot = (n + t) % kRowsScaleSlots;
                 float down_v = 1.f;
+                bool plain = true;   // fp8: one positive scale for every 8 tokens
                 const bool edge = tok0 < all_lo || tok0 + kRowsTile > all_hi;   // the same for all 128 threads
-                if (FP8)
+                if (FP8) {
                     mbar_wait(smem_addr(&sh.scale_full[slot]), ((n + t) / kRowsScaleSlots) & 1u, abort_flag, R.error, 0x822u,
                               R.wait_limit_ns);
+                    plain = sh.plain[slot] != 0u;
+                    vref = sh.vref[slot];
+                    down_v = sh.vdown[slot];
+                }
                 float top4[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
                 auto half_done = [&](int c0) {
-                    if (FP8) {
-                        const float4 *ks = reinterpret_cast<const float4 *>(sh.ks[slot]);
+                    if (FP8 && !plain) {
+                        const float2 *ks = reinterpret_cast<const float2 *>(sh.ks[slot]);
 #pragma unroll
-                        for (int c = c0 / 2; c < c0 / 2 + 16; ++c) {
-                            const float4 f = ks[c];
-                            s[2 * c] = mul2(s[2 * c], make_float2(f.x, f.y));
-                            s[2 * c + 1] = mul2(s[2 * c + 1], make_float2(f.z, f.w));
-                        }
+                        for (int c = c0; c < c0 + 32; ++c) s[c] = mul2(s[c], ks[c]);
                     }
                     if (edge) {
 #pragma unroll
@@ -934,8 +985,18 @@ __device__ __forceinline__ void rows_softmax(const RowsParams &R, RowsShared &sh
                             if (tok0 + 2 * c + 1 < lo || tok0 + 2 * c + 1 >= hi) s[c].y = -INFINITY;
                         }
                     }
+                    if (!FP8) {
 #pragma unroll
-                    for (int c = c0; c < c0 + 32; ++c) top4[c & 3] = max3(top4[c & 3], s[c].x, s[c].y);
+                        for (int c = c0; c < c0 + 32; ++c) top4[c & 3] = max3(top4[c & 3], s[c].x, s[c].y);
+                    } else {
+#pragma unroll
+                        for (int g = c0 / 4; g < c0 / 4 + 8; ++g) {
+                            float x = max3(fmaxf(s[4 * g].x, s[4 * g].y), s[4 * g + 1].x, s[4 * g + 1].y);
+                            x = max3(max3(x, s[4 * g + 2].x, s[4 * g + 2].y), s[4 * g + 3].x, s[4 * g + 3].y);
+                            if (x != -INFINITY && plain) x *= sh.ks8[slot][g];
+                            top4[g & 3] = fmaxf(top4[g & 3], x);
+                        }
+                    }
                 };
                 half_done(0);
                 tc_wait_ld();
@@ -943,11 +1004,7 @@ __device__ __forceinline__ void rows_softmax(const RowsParams &R, RowsShared &sh
                 if (edge) {
                     const uint32_t vu = 2u * (n + t) + 1u;
                     mbar_wait(smem_addr(&sh.full[vu % C::STAGES]), (vu / C::STAGES) & 1u, abort_flag, R.error, 0x823u, R.wait_limit_ns);
-                    clean_values<FP8, DP>(sh, smem_ptr + C::KV_OFF + (vu % C::STAGES) * C::TILE_BYTES, tok0, w.lo, w.hi, r);
-                }
-                if (FP8) {
-                    vref = sh.vref[slot];
-                    down_v = sh.vdown[slot];
+                    clean_values<FP8, DP>(w, smem_ptr + C::KV_OFF + (vu % C::STAGES) * C::TILE_BYTES, tok0, w.lo, w.hi, r);
                 }
                 const float top = fmaxf(fmaxf(top4[0], top4[1]), fmaxf(top4[2], top4[3]));
                 const float x = top * mul;
@@ -971,40 +1028,55 @@ __device__ __forceinline__ void rows_softmax(const RowsParams &R, RowsShared &sh
                     }
                 }
                 const float ref = m == -INFINITY ? 0.f : -m;
-                const float2 mul_2 = make_float2(mul, mul), ref_2 = make_float2(ref, ref);
+                const float2 ref_2 = make_float2(ref, ref);
 #pragma unroll
                 for (int c4 = 0; c4 < 4; ++c4) {
                     uint32_t pk[16];
+                    float2 mul_2 = make_float2(mul, mul);
 #pragma unroll
                     for (int c = 0; c < 16; ++c) {
+                        if (FP8 && (c & 3) == 0) {
+                            const float f = plain ? fmaxf(mul * sh.ks8[slot][4 * c4 + c / 4], 1e-37f) : mul;   // 0 * -infinity: none
+                            mul_2 = make_float2(f, f);
+                        }
                         float2 e = fma2(s[16 * c4 + c], mul_2, ref_2);
                         e.x = fast_exp2(e.x);
                         e.y = fast_exp2(e.y);
                         sum[c & 1] = add2(sum[c & 1], e);
                         if (FP8) {
-                            const float2 v = reinterpret_cast<const float2 *>(sh.vs[slot])[16 * c4 + c];
-                            const float2 y = mul2(e, v);
-                            // a masked token stays 0 whatever its scale is
-                            pk[c] = f16x2(e.x == 0.f ? 0.f : y.x, e.y == 0.f ? 0.f : y.y);
+                            float2 y;
+                            if (plain) {
+                                const float f = sh.vs8[slot][4 * c4 + c / 4];
+                                y = mul2(e, make_float2(f, f));
+                            } else {
+                                y = mul2(e, reinterpret_cast<const float2 *>(sh.vs[slot])[16 * c4 + c]);
+                                if (e.x == 0.f) y.x = 0.f;   // a masked token stays 0 whatever its scale is
+                                if (e.y == 0.f) y.y = 0.f;
+                            }
+                            pk[c] = f16x2(y.x, y.y);
                         } else {
                             pk[c] = bf16x2(e.x, e.y);
                         }
                     }
                     tc_st16(s_at + 16u * c4, pk);
+                    if (c4 & 1) {
+                        tc_wait_st();
+                        tc_fence_before();
+                        __syncwarp();
+                        if (lane == 0) mbar_arrive(smem_addr(c4 == 1 ? &sh.p_half[i] : &sh.p_full[i]));
+                    }
                 }
-                tc_wait_st();
-                tc_fence_before();
-                __syncwarp();
-                if (lane == 0) mbar_arrive(smem_addr(&sh.p_full[i]));
             }
             l = (sum[0].x + sum[0].y) + (sum[1].x + sum[1].y);
-            if (ok) {
-                ok = mbar_wait(smem_addr(&sh.o_full[i]), o_phase & 1u, abort_flag, R.error, 0x824u, R.wait_limit_ns);
-                ++o_phase;
-                ok = __all_sync(0xffffffffu, ok);
-            }
         }
-        named_sync(3, 256);   // both tiles are through: bad_lo and bad_hi are final
+        // the next part's queries go in while this one's last products run
+        more = next_part(part_no + 1u);
+        if (more) next_mul = queries(sh.part[(part_no + 1u) % kRowsParts]);
+        if (active && ok) {
+            ok = mbar_wait(smem_addr(&sh.o_full[i]), o_phase & 1u, abort_flag, R.error, 0x824u, R.wait_limit_ns);
+            ++o_phase;
+            ok = __all_sync(0xffffffffu, ok);
+        }
         uint64_t lse_at;
         __nv_bfloat16 *out = row_out(P, w.q0, w.h, w.blk * kRowsBlock + (live ? prow : 0), lse_at);
         float *part = P.parts + (uint64_t)(2u * blockIdx.x + (w.starts ? 1u : 0u)) * C::PART_FLOATS;
@@ -1013,23 +1085,15 @@ __device__ __forceinline__ void rows_softmax(const RowsParams &R, RowsShared &sh
             if (sh.missing[part_no % kRowsPartSlots]) l = __int_as_float(0x7fc00000);
             const float back = FP8 ? vref * (1.f / C::kUp) : 1.f;
             const float inv = !w.whole ? back : l == 0.f ? 0.f : back / l;
-            const bool bad = sh.bad_lo < sh.bad_hi;
+            const int bad_lo = w.bad_lo, bad_hi = w.bad_hi;
 #pragma unroll 1
             for (int c = 0; c < DP / 32; ++c) {
                 float o[32];
                 __syncwarp();
                 tc_ld32(reinterpret_cast<uint32_t *>(o), o_at + 32u * c);
                 tc_wait_ld();
-                if (bad) {
-                    // by way of the query tile, which nobody needs any more: dimension-major, so that threads do not meet
-                    float *room = reinterpret_cast<float *>(smem_ptr + C::Q_OFF) + prow;
-#pragma unroll
-                    for (int e = 0; e < 32; ++e) room[e * kRowsBlock] = o[e];
-                    if (live) add_not_finite<FP8>(P, w.s, w.h, max(sh.bad_lo, lo), min(sh.bad_hi, hi), 32 * c, room);
-#pragma unroll
-                    for (int e = 0; e < 32; ++e) o[e] = room[e * kRowsBlock];
-                }
                 if (!live) continue;
+                if (bad_lo < bad_hi) add_not_finite<FP8>(P, w, max(bad_lo, lo), min(bad_hi, hi), 32 * c, o);
                 if (w.whole) {
                     store_row(P, out, 32 * c, o, inv);
                 } else {
@@ -1049,20 +1113,22 @@ __device__ __forceinline__ void rows_softmax(const RowsParams &R, RowsShared &sh
             }
             tc_fence_before();
         }
-        if (!w.whole) {
-            const uint32_t more = w.c1 - w.c0;
-            if (R.join && more >= kRowsHere) {
-                if (tid == 0 && w.starts) R.join[blockIdx.x] = RowsJoin{more + 1u, w.s, w.blk, w.h};
+        if (!w.whole && active) {
+            const uint32_t others = w.c1 - w.c0;
+            if (R.join && others >= kRowsHere) {
+                if (tid == 0 && w.starts) R.join[blockIdx.x] = RowsJoin{others + 1u, w.s, w.blk, w.h};
             } else {
+                // the two tiles of a block are joined each by itself
                 __threadfence();
-                named_sync(3, 256);
-                if (tid == 0) {
-                    const uint32_t seen = atomicAdd(P.counters + w.c0, 1u);
-                    sh.last = seen == more;
-                    if (seen == more) P.counters[w.c0] = 0u;  // ready for the next call
+                named_sync(3 + i, 128);
+                if (r == 0) {
+                    uint32_t *counter = P.counters + 2u * w.c0 + i;
+                    const uint32_t seen = atomicAdd(counter, 1u);
+                    sh.last[i] = seen == others;
+                    if (seen == others) *counter = 0u;  // ready for the next call
                 }
-                named_sync(3, 256);
-                if (sh.last && live) {
+                named_sync(3 + i, 128);
+                if (sh.last[i] && live) {
                     __threadfence();
                     float jm, jl;
 #pragma unroll 1
@@ -1076,6 +1142,8 @@ __device__ __forceinline__ void rows_softmax(const RowsParams &R, RowsShared &sh
             }
         }
         n += nt;
+        __syncwarp();
+        if (lane == 0) mbar_arrive(smem_addr(&sh.part_empty[part_no % kRowsParts]));
     }
 }
 
@@ -1106,13 +1174,13 @@ __global__ void __launch_bounds__(kRowsThreads, 1) attend_rows_kernel(const __gr
     const AttendParams &P = R.a;
     extern __shared__ uint8_t smem_raw[];
     __shared__ RowsShared sh;
-    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+    const int tid = threadIdx.x, warp = __shfl_sync(0xffffffffu, tid >> 5, 0), lane = tid & 31;
     uint8_t *smem_ptr = smem_raw + ((1024u - (smem_addr(smem_raw) & 1023u)) & 1023u);
     const uint32_t smem = smem_addr(smem_ptr);
     if (R.join && tid == 0) R.join[blockIdx.x].parts = 0u;   // tid 0 also enters a block there
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
 
-    // the length of the line of tiles
+    // the length of the line
     long long total = 0;
     for (uint32_t s0 = 0; s0 < P.seqs.n_seqs; s0 += kRowsThreads) {
         const uint32_t s = s0 + tid;
@@ -1163,7 +1231,7 @@ __global__ void __launch_bounds__(kRowsThreads, 1) attend_rows_kernel(const __gr
         long long off = begin - sh.before;
         for (int b0 = 0; b0 < w.blocks; b0 += 32) {
             const int b = b0 + lane;
-            const long long n = b < w.blocks ? (long long)rows_span(P, w, b).tiles * P.cache.H : 0;
+            const long long n = b < w.blocks ? (long long)(rows_span(P, w, b).tiles + kRowsCost) * P.cache.H : 0;
             long long incl = n;
 #pragma unroll
             for (int o = 1; o < 32; o <<= 1) {
@@ -1173,10 +1241,10 @@ __global__ void __launch_bounds__(kRowsThreads, 1) attend_rows_kernel(const __gr
             const bool here = off >= incl - n && off < incl;
             if (here) {
                 const long long in = off - (incl - n);
-                const int tiles = rows_span(P, w, b).tiles;
+                const int units = rows_span(P, w, b).tiles + kRowsCost;
                 sh.blk = b;
-                sh.h = (int)(in / tiles);
-                sh.tile = (int)(in % tiles);
+                sh.h = (int)(in / units);
+                sh.unit = (int)(in % units);
             }
             if (__any_sync(0xffffffffu, here)) break;
             off -= __shfl_sync(0xffffffffu, incl, 31);
@@ -1194,10 +1262,15 @@ __global__ void __launch_bounds__(kRowsThreads, 1) attend_rows_kernel(const __gr
         for (int i = 0; i < 2; ++i) {
             mbar_init(smem_addr(&sh.q_full[i]), 4);
             mbar_init(smem_addr(&sh.s_full[i]), 1);
+            mbar_init(smem_addr(&sh.p_half[i]), 4);
             mbar_init(smem_addr(&sh.p_full[i]), 4);
             mbar_init(smem_addr(&sh.o_full[i]), 1);
         }
         for (int i = 0; i < kRowsScaleSlots; ++i) mbar_init(smem_addr(&sh.scale_full[i]), 4);
+        for (int i = 0; i < kRowsParts; ++i) {
+            mbar_init(smem_addr(&sh.part_full[i]), 1);
+            mbar_init(smem_addr(&sh.part_empty[i]), 8);
+        }
         mbar_init(smem_addr(&sh.drained), 1);
         sh.abort_flag = 0u;
         for (int i = 0; i < kRowsPartSlots; ++i) sh.missing[i] = 0u;
@@ -1219,11 +1292,13 @@ __global__ void __launch_bounds__(kRowsThreads, 1) attend_rows_kernel(const __gr
     k.blk = sh.blk;
     k.h = sh.h;
     k.sp = rows_span(P, k.w, k.blk);
-    k.left = (int)(end - begin);
-    k.t0 = sh.tile;
-    k.t1 = min(k.sp.tiles, k.t0 + k.left);
+    k.reach = end - (begin - sh.unit + kRowsCost);
+    k.t0 = max(0, sh.unit - kRowsCost);
+    k.t1 = (int)min((long long)k.sp.tiles, k.reach);
+    const bool any = k.t1 > k.t0;   // the stretch may lie in a block's extra units altogether
 
-    if (warp < 8) {
+    if (!any) {
+    } else if (warp < 8) {
         asm volatile("setmaxnreg.inc.sync.aligned.u32 200;");
         rows_softmax<FP8, DP>(R, sh, smem_ptr, smem, tmem, warp >> 2, tid);
     } else if (warp < 12) {
@@ -1232,15 +1307,16 @@ __global__ void __launch_bounds__(kRowsThreads, 1) attend_rows_kernel(const __gr
         else if (FP8) rows_convert<DP>(R, sh, k, smem_ptr, smem, tid - 256);
     } else {
         asm volatile("setmaxnreg.dec.sync.aligned.u32 48;");
-        if (tid == 12 * 32) {
-            rows_mma<FP8, DP>(R, sh, k, smem, tmem);
+        if (warp == 12) {
+            rows_mma<FP8, DP>(R, sh, k, __shfl_sync(0xffffffffu, smem, 0), __shfl_sync(0xffffffffu, tmem, 0));
             // whatever has been issued ends before the tensor memory is given back
             tc_commit(smem_addr(&sh.drained));
             mbar_drain(smem_addr(&sh.drained), 0u, 4ull * R.wait_limit_ns);
         } else if (warp == 13 && R.tma) {
             rows_fetch<FP8, DP>(R, sh, k, smem, lane);
         } else if (warp == 14) {
-            rows_parts(R, sh, k, begin, ctas, lane);
+            if (lane == 0) rows_parts(R, sh, k, end, ctas);
+            __syncwarp();
         }
         __syncwarp();
     }
