@@ -35,6 +35,7 @@ constexpr int kRowsThreads = 512;
 constexpr int kRowsRaw = 3;                  // fp8 tiles in flight
 constexpr int kRowsScaleSlots = 4;
 constexpr int kRowsGroup = 8;                // tokens that share a scale wherever tensor copies are used
+static_assert(2 * kRowsTile / kRowsGroup == 32, "a lane for each");
 constexpr int kRowsParts = 4;                // parts that the softmax warps may know of at a time
 constexpr int kRowsPartSlots = 16;           // more than the parts between the first and the last role
 
@@ -276,7 +277,7 @@ struct RowsShared {
     long long row_at[2][kRowsTile];  // byte offset of each token of a tile, or -1
     uint32_t missing[kRowsPartSlots];             // a page that the table should have held is missing: by part, in turn
     float ks[kRowsScaleSlots][kRowsTile], vs[kRowsScaleSlots][kRowsTile];
-    float ks8[kRowsScaleSlots][kRowsTile / kRowsGroup], vs8[kRowsScaleSlots][kRowsTile / kRowsGroup];
+    float kv8[kRowsScaleSlots][2 * kRowsTile / kRowsGroup];   // K scales of the groups, then V scales: a lane each
     float vref[kRowsScaleSlots], vdown[kRowsScaleSlots], vtop[2][4];
     uint32_t plain[kRowsScaleSlots], odd[2][4];   // scales are equal within groups, positive and finite
 };
@@ -435,16 +436,22 @@ __device__ __forceinline__ void rows_convert(const RowsParams &R, RowsShared &sh
     const int lane = tid & 31, warp = tid >> 5;
     RowsAt a{k, k.t0, 0u, true};
     float ks = 0.f, vs = 0.f;   // of this thread's token in the tile at `a`
-    auto look_up = [&]() {
-        ks = vs = 0.f;
+    int g = -1;                 // its page
+    // two loads that depend on each other, with a unit's conversion after each: nobody waits for them
+    auto look_up_page = [&]() {
         const int tok = a.k.sp.first + a.t * kRowsTile + tid;
-        if (!a.more || tok < a.k.sp.lo || tok >= a.k.sp.hi || a.k.w.bad) return;
-        const int g = __ldg(P.seqs.page_table + (uint64_t)a.k.s * P.seqs.table_stride + P.cache.by_T.div((uint32_t)tok));
+        g = -1;
+        if (a.more && tok >= a.k.sp.lo && tok < a.k.sp.hi && !a.k.w.bad)
+            g = __ldg(P.seqs.page_table + (uint64_t)a.k.s * P.seqs.table_stride + P.cache.by_T.div((uint32_t)tok));
+    };
+    auto look_up_scales = [&]() {
+        ks = vs = 0.f;
         if ((uint32_t)g >= P.cache.num_pages) return;
         ks = __ldg(P.cache.ks + (uint64_t)g * P.cache.s_page + a.k.h);
         vs = __ldg(P.cache.vs + (uint64_t)g * P.cache.s_page + a.k.h);
     };
-    look_up();
+    look_up_page();
+    look_up_scales();
     float vref = 0.f;
     uint32_t part = 0xffffffffu, unit = 0;
     bool ok = true;
@@ -479,8 +486,8 @@ __device__ __forceinline__ void rows_convert(const RowsParams &R, RowsShared &sh
             vg = fmaxf(vg, __shfl_xor_sync(0xffffffffu, vg, o));
         }
         if (lane % kRowsGroup == 0) {
-            sh.ks8[slot][tid / kRowsGroup] = kg;
-            sh.vs8[slot][tid / kRowsGroup] = vg;
+            sh.kv8[slot][tid / kRowsGroup] = kg;
+            sh.kv8[slot][kRowsTile / kRowsGroup + tid / kRowsGroup] = vg;
         }
         if (tid == 0) {
             sh.vref[slot] = vref;
@@ -490,9 +497,10 @@ __device__ __forceinline__ void rows_convert(const RowsParams &R, RowsShared &sh
         __syncwarp();
         if (lane == 0) mbar_arrive(smem_addr(&sh.scale_full[slot]));
         at_next(P, a);
-        look_up();
+        look_up_page();
 #pragma unroll 1
         for (int kv = 0; kv < 2; ++kv, ++unit) {
+            if (kv == 1) look_up_scales();
             const uint32_t rs = unit % kRowsRaw, st = unit % C::STAGES;
             ok = ok && mbar_wait(smem_addr(&sh.raw_full[rs]), (unit / kRowsRaw) & 1u, abort_flag, R.error, 0x803u, R.wait_limit_ns);
             if (unit >= C::STAGES)
@@ -656,7 +664,6 @@ __device__ __forceinline__ void rows_mma(const RowsParams &R, RowsShared &sh, Ro
         const int nt = k.t1 - k.t0;
         for (int t = 0; t <= nt; ++t) {
             const uint32_t n = tile_no + t, u = 2u * n;  // K's place among the loaded tiles
-            if (t < nt && !wait(&sh.full[u % C::STAGES], (u / C::STAGES) & 1u, 0x811u)) return;
             if (t > 0 && !wait(&sh.full[(u - 1u) % C::STAGES], ((u - 1u) / C::STAGES) & 1u, 0x812u)) return;
             for (int i = 0; i < act; ++i) {
                 if (t > 0) {
@@ -670,6 +677,7 @@ __device__ __forceinline__ void rows_mma(const RowsParams &R, RowsShared &sh, Ro
                     if (t == nt) tc_commit(smem_addr(&sh.o_full[i]));
                 }
                 if (t < nt) {
+                    if (i == 0 && !wait(&sh.full[u % C::STAGES], (u / C::STAGES) & 1u, 0x811u)) return;
                     if (t == 0) {
                         if (!wait(&sh.q_full[i], q_phase[i] & 1u, 0x814u)) return;
                         ++q_phase[i];
@@ -692,42 +700,45 @@ __device__ __forceinline__ void rows_mma(const RowsParams &R, RowsShared &sh, Ro
     } while (walk_next(P, k));
 }
 
-// This thread's query row into shared memory, as f16 (fp8 caches, divided by a power of two that is returned) or bf16.
+// A warp's 32 query rows (from block row `row0` on) into shared memory, as bf16 or, for fp8 caches, as f16 divided by each
+// row's power of two, which the row's own lane gets back.  DP / 8 lanes share a row, so that loads are whole lines.
 template <bool FP8, int DP>
-__device__ __forceinline__ float rows_query(const RowsParams &R, const RowsPart &w, uint32_t dst, int r, int row, bool live)
+__device__ __forceinline__ float rows_query(const RowsParams &R, const RowsPart &w, uint32_t dst, int row0, int lane)
 {
     const AttendParams &P = R.a;
-    float up = 1.f;
-    const uint32_t j = P.by_G.div((uint32_t)(live ? row : 0));
-    const uint32_t head = (uint32_t)w.h * P.G + (uint32_t)((live ? row : 0) - (int)(j * P.G));
-    const __nv_bfloat16 *p = P.q + (uint64_t)(w.q0 + (int)j) * P.q_tok + (uint64_t)head * P.q_head;
-    const uint32_t pieces = P.cache.D / 8u;
-    float down = R.q_sign;
-    uint4 x[DP / 8];
+    constexpr int LPR = DP / 8, RPI = 32 / LPR;   // lanes of a row, rows of a load
+    const uint32_t c = (uint32_t)lane % LPR;
+    const int sub = lane / LPR;
+    float up_mine = 1.f;
+    uint4 x[32 / RPI];
 #pragma unroll
-    for (uint32_t c = 0; c < DP / 8; ++c) {
-        x[c] = make_uint4(0u, 0u, 0u, 0u);
-        if (live && c < pieces) x[c] = __ldg(reinterpret_cast<const uint4 *>(p) + c);
+    for (int k = 0; k < 32 / RPI; ++k) {
+        const int br = row0 + k * RPI + sub;
+        const uint32_t row = (uint32_t)(w.blk * kRowsBlock + br), j = P.by_G.div(row);
+        const uint32_t head = (uint32_t)w.h * P.G + (row - j * P.G);
+        x[k] = make_uint4(0u, 0u, 0u, 0u);
+        if (br < w.rows && 8u * c < P.cache.D)
+            x[k] = __ldg(reinterpret_cast<const uint4 *>(P.q + (uint64_t)(w.q0 + (int)j) * P.q_tok + (uint64_t)head * P.q_head) + c);
     }
-    if (FP8) {
-        uint32_t top = 0;
 #pragma unroll
-        for (uint32_t c = 0; c < DP / 8; ++c) {
-            const uint32_t y[4] = {x[c].x, x[c].y, x[c].z, x[c].w};
+    for (int k = 0; k < 32 / RPI; ++k) {
+        uint32_t y[4] = {x[k].x, x[k].y, x[k].z, x[k].w};
+        float down = R.q_sign;
+        if (FP8) {
+            uint32_t top = 0;
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
                 const uint32_t a = y[e] & 0x7fffu, b = (y[e] >> 16) & 0x7fffu;
                 if (a < 0x7f80u) top = max(top, a);
                 if (b < 0x7f80u) top = max(top, b);
             }
-        }
-        const int ex = min(max((int)(top >> 7) - 127, -126), 126);
-        down *= __uint_as_float((uint32_t)(127 - ex) << 23);
-        up = __uint_as_float((uint32_t)(127 + ex) << 23);
-    }
 #pragma unroll
-    for (uint32_t c = 0; c < DP / 8; ++c) {
-        uint32_t y[4] = {x[c].x, x[c].y, x[c].z, x[c].w};
+            for (int o = 1; o < LPR; o <<= 1) top = max(top, __shfl_xor_sync(0xffffffffu, top, o));
+            const int ex = min(max((int)(top >> 7) - 127, -126), 126);
+            down *= __uint_as_float((uint32_t)(127 - ex) << 23);
+            const float up = __shfl_sync(0xffffffffu, __uint_as_float((uint32_t)(127 + ex) << 23), (lane % RPI) * LPR);
+            if (lane / RPI == k) up_mine = up;
+        }
         if (FP8 || R.q_sign != 1.f) {
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
@@ -735,9 +746,9 @@ __device__ __forceinline__ float rows_query(const RowsParams &R, const RowsPart 
                 y[e] = FP8 ? f16x2(a, b) : bf16x2(a, b);
             }
         }
-        sts16(dst + tc_piece(r, c), y[0], y[1], y[2], y[3]);
+        sts16(dst + tc_piece((uint32_t)((row0 + k * RPI + sub) & (kRowsTile - 1)), c), y[0], y[1], y[2], y[3]);
     }
-    return up;
+    return up_mine;
 }
 
 // One thread: the parts of the stretch, ahead of the softmax warps.
@@ -795,45 +806,78 @@ __device__ __forceinline__ __nv_bfloat16 *row_out(const AttendParams &P, int q0,
     return P.out + (uint64_t)(q0 + (int)j) * P.o_tok + (uint64_t)head * P.o_head;
 }
 
+// the largest of three, NaN if one of them is
 __device__ __forceinline__ float max3(float a, float b, float c)
 {
     float d;
-    asm("max.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(b), "f"(c));
+    asm("max.NaN.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(b), "f"(c));
     return d;
+}
+__device__ __forceinline__ float max2(float a, float b)
+{
+    float d;
+    asm("max.NaN.f32 %0, %1, %2;" : "=f"(d) : "f"(a), "f"(b));
+    return d;
+}
+
+// 2^x of two values on the arithmetic pipes, so that the special-function pipe does not bound the softmax: x = n + f with
+// n the nearest whole number, 2^f by a polynomial of degree 4 with p(0) = 1 (least largest relative error on [-1/2, 1/2]:
+// 2.8e-6), n added to the exponent.  At -127 and below the result is 0.
+__device__ __forceinline__ float2 poly_exp2(float2 x)
+{
+    x.x = fmaxf(x.x, -127.f);
+    x.y = fmaxf(x.y, -127.f);
+    const float magic = 12582912.f;   // 1.5 * 2^23: adding it rounds to a whole number, which its low bits then hold
+    const float2 t = add2(x, make_float2(magic, magic));
+    const float2 n = add2(t, make_float2(-magic, -magic));
+    const float2 f = fma2(n, make_float2(-1.f, -1.f), x);
+    float2 p = fma2(f, make_float2(0.009582852944731712f, 0.009582852944731712f), make_float2(0.055906426161527634f, 0.055906426161527634f));
+    p = fma2(p, f, make_float2(0.24024099111557007f, 0.24024099111557007f));
+    p = fma2(p, f, make_float2(0.6931241750717163f, 0.6931241750717163f));
+    p = fma2(p, f, make_float2(1.f, 1.f));
+    return make_float2(__int_as_float(__float_as_int(p.x) + (__float_as_int(t.x) << 23)),
+                       __int_as_float(__float_as_int(p.y) + (__float_as_int(t.y) << 23)));
 }
 
 // 0 * infinity must not reach rows that do not attend to a token, so infinities and NaN of a V tile become 0 here;
 // bad_lo and bad_hi tell the end of the part where to look for those that some row does attend to.
 template <bool FP8, int DP>
-__device__ __noinline__ void clean_values(RowsPart &part, uint8_t *v, int tok0, int lo, int hi, int r)
+__device__ __forceinline__ void clean_values(RowsPart &part, uint8_t *v, int tok0, int lo, int hi, int r)
 {
+    constexpr uint32_t E = FP8 ? 0x7c00u : 0x7f80u;
+    constexpr int N = RowsCfg<FP8, DP>::TILE_BYTES / 16 / 128;
+    uint4 x[N];
+#pragma unroll
+    for (int k = 0; k < N; ++k) x[k] = *reinterpret_cast<const uint4 *>(v + 16 * (r + 128 * k));
     bool found = false;
-    for (int c = r; c < RowsCfg<FP8, DP>::TILE_BYTES / 16; c += 128) {
+#pragma unroll
+    for (int k = 0; k < N; ++k) {
+        const uint32_t y[4] = {x[k].x, x[k].y, x[k].z, x[k].w};
+#pragma unroll
+        for (int e = 0; e < 4; ++e) found |= (y[e] & E) == E || (y[e] & (E << 16)) == (E << 16);
+    }
+    if (!found) return;
+#pragma unroll 1
+    for (int c = r; c < 128 * N; c += 128) {
         uint32_t *w = reinterpret_cast<uint32_t *>(v + 16 * c);
-        const uint4 x = *reinterpret_cast<const uint4 *>(w);
-        const uint32_t y[4] = {x.x, x.y, x.z, x.w};
-        constexpr uint32_t E = FP8 ? 0x7c00u : 0x7f80u;
         bool hit = false;
 #pragma unroll
-        for (int e = 0; e < 4; ++e) hit |= (y[e] & E) == E || (y[e] & (E << 16)) == (E << 16);
-        if (hit) {
-            found = true;
+        for (int e = 0; e < 4; ++e) {
+            uint32_t z = w[e];
+            if ((z & E) == E) z &= 0xffff0000u;
+            if ((z & (E << 16)) == (E << 16)) z &= 0xffffu;
+            if (z == w[e]) continue;
             const int tok = tok0 + (c & (8 * kRowsTile - 1)) / 8;
-            if (tok >= lo && tok < hi) {   // others are nobody's: the rest of a page, or never loaded
+            if (!hit && tok >= lo && tok < hi) {   // others are nobody's: the rest of a page, or never loaded
                 atomicMin(&part.bad_lo, tok);
                 atomicMax(&part.bad_hi, tok + 1);
                 __threadfence_block();
             }
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                uint32_t z = y[e];
-                if ((z & E) == E) z &= 0xffff0000u;
-                if ((z & (E << 16)) == (E << 16)) z &= 0xffffu;
-                w[e] = z;
-            }
+            hit = true;
+            w[e] = z;
         }
     }
-    if (found) fence_async_smem();
+    fence_async_smem();
 }
 
 // Infinities and NaN that the products left out, added to 32 outputs of a row that attends to [lo, hi) of them.
@@ -885,17 +929,179 @@ __device__ __forceinline__ void join_row(const float *parts, uint32_t c0, uint32
     }
 }
 
-__device__ __forceinline__ void store_row(const AttendParams &P, __nv_bfloat16 *out, int d, const float (&v)[32], float f)
+__device__ __forceinline__ float lse_of(float m, float l) { return l == 0.f ? -INFINITY : m * 0.69314718055994531f + logf(l); }
+
+// What a thread keeps of its row.
+struct RowState {
+    float m;         // reference of the exponentials; no score is more than kRise above it
+    float2 sum[2];
+    float mul;       // scale * log2(e), times the row's power of two with f16 queries
+    int lo, hi;      // tokens that the row attends to
+};
+
+// One tile of scores to weights, in tensor memory.  PLAIN (fp8): one scale, positive and finite, for every 8 tokens.
+//
+// Two passes over the scores, 32 at a time with the next 32 on their way: the maximum, then the weights.  Keeping all
+// 128 in registers saves the second read but unrolls the tile into more code than the instruction cache holds beside
+// the other roles' (fp8: 2.8 of 10 stall cycles per instruction were fetches).  The weights of the first two chunks lie in columns
+// of chunk 0, and so on: no score is overwritten before it has been read.
+template <bool FP8, bool PLAIN, int DP>
+__device__ __forceinline__ void soft_tile(RowsShared &sh, RowState &S, uint32_t s_at, uint32_t o_at, uint32_t slot, int tok0, bool edge,
+                                          bool first, float down_v, float scales, uint32_t half_bar, uint32_t full_bar, int lane)
 {
+    using C = RowsCfg<FP8, DP>;
+    float2 a[16], b[16];
+    // the chunk's scores, scaled (one scale per token) and masked
+    auto settle = [&](float2 (&s)[16], int c) {
+        if (FP8 && !PLAIN) {
+            const float2 *ks = reinterpret_cast<const float2 *>(sh.ks[slot]) + 16 * c;
 #pragma unroll
-    for (int e = 0; e < 32; e += 8)
-        if (d + e < (int)P.cache.D)
-            *reinterpret_cast<uint4 *>(out + d + e) =
-                make_uint4(bf16x2(v[e] * f, v[e + 1] * f), bf16x2(v[e + 2] * f, v[e + 3] * f), bf16x2(v[e + 4] * f, v[e + 5] * f),
-                           bf16x2(v[e + 6] * f, v[e + 7] * f));
+            for (int e = 0; e < 16; ++e) s[e] = mul2(s[e], ks[e]);
+        }
+        if (edge) {
+            const int lo = S.lo - tok0 - 32 * c, hi = S.hi - tok0 - 32 * c;   // columns [lo, hi) count
+            uint32_t seen = hi >= 32 ? 0xffffffffu : hi <= 0 ? 0u : (1u << hi) - 1u;
+            seen &= lo <= 0 ? 0xffffffffu : lo >= 32 ? 0u : ~((1u << lo) - 1u);
+#pragma unroll
+            for (int e = 0; e < 16; ++e) {
+                if (!(seen & (1u << (2 * e)))) s[e].x = -INFINITY;
+                if (!(seen & (2u << (2 * e)))) s[e].y = -INFINITY;
+            }
+        }
+    };
+    float top4[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+    auto largest = [&](float2 (&s)[16], int c) {
+        settle(s, c);
+        if (!FP8 || !PLAIN) {
+#pragma unroll
+            for (int e = 0; e < 16; ++e) top4[e & 3] = max3(top4[e & 3], s[e].x, s[e].y);
+        } else {
+#pragma unroll
+            for (int g = 0; g < 4; ++g) {
+                float x = max3(max2(s[4 * g].x, s[4 * g].y), s[4 * g + 1].x, s[4 * g + 1].y);
+                x = max3(max3(x, s[4 * g + 2].x, s[4 * g + 2].y), s[4 * g + 3].x, s[4 * g + 3].y);
+                const float f = __shfl_sync(0xffffffffu, scales, 4 * c + g);
+                top4[g] = max2(top4[g], x == -INFINITY ? x : x * f);
+            }
+        }
+    };
+    tc_ld32(reinterpret_cast<uint32_t *>(a), s_at);
+#pragma unroll 1
+    for (int c = 0; c < 4; c += 2) {
+        tc_wait_ld();
+        tc_ld32(reinterpret_cast<uint32_t *>(b), s_at + 32u * (c + 1));
+        largest(a, c);
+        tc_wait_ld();
+        tc_ld32(reinterpret_cast<uint32_t *>(a), s_at + 32u * ((c + 2) & 3));   // in the end the first again
+        largest(b, c + 1);
+    }
+    const float top = max2(max2(top4[0], top4[1]), max2(top4[2], top4[3]));
+    const float x = top * S.mul;
+    if (first) {
+        S.m = top == -INFINITY ? -INFINITY : x;
+    } else if (__any_sync(0xffffffffu, x > S.m + C::kRise || (FP8 && down_v != 1.f))) {
+        const float nm = x > S.m ? x : S.m;
+        const float f = nm == S.m ? 1.f : fast_exp2(S.m - nm);
+        S.m = nm;
+        S.sum[0] = mul2(S.sum[0], make_float2(f, f));
+        S.sum[1] = mul2(S.sum[1], make_float2(f, f));
+        const float g = f * down_v;
+#pragma unroll 1
+        for (int c = 0; c < DP / 16; ++c) {
+            uint32_t o[16];
+            tc_ld16(o, o_at + 16u * c);
+            tc_wait_ld();
+#pragma unroll
+            for (int e = 0; e < 16; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * g);
+            tc_st16(o_at + 16u * c, o);
+        }
+    }
+    const float ref = S.m == -INFINITY ? 0.f : -S.m;
+    const float2 ref_2 = make_float2(ref, ref);
+    auto weights = [&](float2 (&s)[16], int c) {
+        settle(s, c);
+        uint32_t pk[16];
+        float2 mul_2 = make_float2(S.mul, S.mul);
+        float fv = 1.f;
+#pragma unroll
+        for (int e = 0; e < 16; ++e) {
+            if (FP8 && PLAIN && (e & 3) == 0) {
+                const float f = fmaxf(S.mul * __shfl_sync(0xffffffffu, scales, 4 * c + e / 4), 1e-37f);   // 0 * -infinity: none
+                mul_2 = make_float2(f, f);
+                fv = __shfl_sync(0xffffffffu, scales, 16 + 4 * c + e / 4);
+            }
+            float2 y = fma2(s[e], mul_2, ref_2);
+            if ((e & 3) == 3) {
+                y = poly_exp2(y);
+            } else {
+                y.x = fast_exp2(y.x);
+                y.y = fast_exp2(y.y);
+            }
+            S.sum[e & 1] = add2(S.sum[e & 1], y);
+            if (FP8) {
+                float2 z;
+                if (PLAIN) {
+                    z = mul2(y, make_float2(fv, fv));
+                } else {
+                    z = mul2(y, reinterpret_cast<const float2 *>(sh.vs[slot])[16 * c + e]);
+                    if (y.x == 0.f) z.x = 0.f;   // a masked token stays 0 whatever its scale is
+                    if (y.y == 0.f) z.y = 0.f;
+                }
+                pk[e] = f16x2(z.x, z.y);
+            } else {
+                pk[e] = bf16x2(y.x, y.y);
+            }
+        }
+        tc_st16(s_at + 16u * c, pk);
+    };
+#pragma unroll 1
+    for (int c = 0; c < 4; c += 2) {
+        tc_wait_ld();
+        tc_ld32(reinterpret_cast<uint32_t *>(b), s_at + 32u * (c + 1));
+        weights(a, c);
+        tc_wait_ld();
+        if (c == 0) tc_ld32(reinterpret_cast<uint32_t *>(a), s_at + 64u);
+        weights(b, c + 1);
+        tc_wait_st();
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(c == 0 ? half_bar : full_bar);
+    }
+    if (!(top <= 3.402823466e38f)) S.sum[0].x = __int_as_float(0x7fc00000);   // a score of infinity or NaN: the row is no number
 }
 
-__device__ __forceinline__ float lse_of(float m, float l) { return l == 0.f ? -INFINITY : m * 0.69314718055994531f + logf(l); }
+// 32 outputs of each row of a warp, from dimension d on: four lanes exchange pieces so that they store 64 bytes of
+// one row together.
+__device__ __forceinline__ void store_rows(const AttendParams &P, __nv_bfloat16 *out, bool live, int d, const float (&v)[32], float f,
+                                           int lane)
+{
+    uint4 x[4];
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+        x[e] = make_uint4(bf16x2(v[8 * e] * f, v[8 * e + 1] * f), bf16x2(v[8 * e + 2] * f, v[8 * e + 3] * f),
+                          bf16x2(v[8 * e + 4] * f, v[8 * e + 5] * f), bf16x2(v[8 * e + 6] * f, v[8 * e + 7] * f));
+    const int q = lane & 3;
+    // transpose the 4 x 4 pieces of a quad: first halves, then neighbours
+    auto swap = [&](uint4 &a, uint4 &b, int o, bool up) {   // lanes with `up` keep b and give a
+        uint4 give = up ? a : b;
+        give.x = __shfl_xor_sync(0xffffffffu, give.x, o);
+        give.y = __shfl_xor_sync(0xffffffffu, give.y, o);
+        give.z = __shfl_xor_sync(0xffffffffu, give.z, o);
+        give.w = __shfl_xor_sync(0xffffffffu, give.w, o);
+        if (up) a = give;
+        else b = give;
+    };
+    swap(x[0], x[2], 2, q & 2);
+    swap(x[1], x[3], 2, q & 2);
+    swap(x[0], x[1], 1, q & 1);
+    swap(x[2], x[3], 1, q & 1);
+    const unsigned long long mine = live ? (unsigned long long)(uintptr_t)out : 0ull;
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {   // x[k]: piece q of the row of the quad's lane k
+        __nv_bfloat16 *to = reinterpret_cast<__nv_bfloat16 *>((uintptr_t)__shfl_sync(0xffffffffu, mine, (lane & ~3) | k));
+        if (to && d + 8 * q < (int)P.cache.D) *reinterpret_cast<uint4 *>(to + d + 8 * q) = x[k];
+    }
+}
 
 // Softmax and output of one tile of 128 rows: one thread per row.
 template <bool FP8, int DP>
@@ -920,7 +1126,7 @@ __device__ __forceinline__ void rows_softmax(const RowsParams &R, RowsShared &sh
     auto queries = [&](const RowsPart &w) -> float {
         float mul = R.scale_log2;
         if (i * kRowsTile < w.rows) {
-            mul *= rows_query<FP8, DP>(R, w, smem + C::Q_OFF + i * C::TILE_BYTES, r, w.blk * kRowsBlock + prow, prow < w.rows);
+            mul *= rows_query<FP8, DP>(R, w, smem + C::Q_OFF + i * C::TILE_BYTES, prow & ~31, lane);
             fence_async_smem();
             __syncwarp();
             if (lane == 0) mbar_arrive(smem_addr(&sh.q_full[i]));
@@ -935,34 +1141,22 @@ __device__ __forceinline__ void rows_softmax(const RowsParams &R, RowsShared &sh
         const int nt = w.tiles;
         const bool active = i * kRowsTile < w.rows;
         const bool live = prow < w.rows;
-        const float mul = next_mul;
-        float m = -INFINITY, l = 0.f, vref = 1.f;
-        int lo = 0, hi = 0;
+        RowState S{-INFINITY, {}, next_mul, 0, 0};
+        float vref = 1.f;
         bool ok = true;
         if (active) {
-            if (live) row_span(P, w.at, w.kv, w.blk * kRowsBlock + prow, lo, hi);
+            if (live) row_span(P, w.at, w.kv, w.blk * kRowsBlock + prow, S.lo, S.hi);
             // tokens that every live row of this tile attends to
             int all_lo, all_hi, x0, x1;
             row_span(P, w.at, w.kv, w.blk * kRowsBlock + i * kRowsTile, x0, all_hi);
             row_span(P, w.at, w.kv, w.blk * kRowsBlock + min(w.rows, (i + 1) * kRowsTile) - 1, all_lo, x1);
-            float2 sum[2] = {};
             int tok0 = w.first;
             for (int t = 0; t < nt; ++t, tok0 += kRowsTile) {
-                ok = mbar_wait(smem_addr(&sh.s_full[i]), s_phase & 1u, abort_flag, R.error, 0x821u, R.wait_limit_ns);
-                ++s_phase;
-                ok = __all_sync(0xffffffffu, ok);
-                if (!ok) break;
-                tc_fence_after();
-                float2 s[64];
-                uint32_t *raw = reinterpret_cast<uint32_t *>(s);
-                tc_ld32(raw, s_at);
-                tc_ld32(raw + 32, s_at + 32u);
-                tc_wait_ld();
-                tc_ld32(raw + 64, s_at + 64u);
-                tc_ld32(raw + 96, s_at + 96u);
+                // what shared memory holds is fetched before the scores are there: loads from it are slow while the tensor
+                // cores read their operands
                 const uint32_t slot = (n + t) % kRowsScaleSlots;
-                float down_v = 1.f;
-                bool plain = true;   // fp8: one positive scale for every 8 tokens
+                float down_v = 1.f, scales = 0.f;
+                bool plain = true;
                 const bool edge = tok0 < all_lo || tok0 + kRowsTile > all_hi;   // the same for all 128 threads
                 if (FP8) {
                     mbar_wait(smem_addr(&sh.scale_full[slot]), ((n + t) / kRowsScaleSlots) & 1u, abort_flag, R.error, 0x822u,
@@ -970,105 +1164,25 @@ __device__ __forceinline__ void rows_softmax(const RowsParams &R, RowsShared &sh
                     plain = sh.plain[slot] != 0u;
                     vref = sh.vref[slot];
                     down_v = sh.vdown[slot];
+                    scales = sh.kv8[slot][lane];
                 }
-                float top4[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
-                auto half_done = [&](int c0) {
-                    if (FP8 && !plain) {
-                        const float2 *ks = reinterpret_cast<const float2 *>(sh.ks[slot]);
-#pragma unroll
-                        for (int c = c0; c < c0 + 32; ++c) s[c] = mul2(s[c], ks[c]);
-                    }
-                    if (edge) {
-#pragma unroll
-                        for (int c = c0; c < c0 + 32; ++c) {
-                            if (tok0 + 2 * c < lo || tok0 + 2 * c >= hi) s[c].x = -INFINITY;
-                            if (tok0 + 2 * c + 1 < lo || tok0 + 2 * c + 1 >= hi) s[c].y = -INFINITY;
-                        }
-                    }
-                    if (!FP8) {
-#pragma unroll
-                        for (int c = c0; c < c0 + 32; ++c) top4[c & 3] = max3(top4[c & 3], s[c].x, s[c].y);
-                    } else {
-#pragma unroll
-                        for (int g = c0 / 4; g < c0 / 4 + 8; ++g) {
-                            float x = max3(fmaxf(s[4 * g].x, s[4 * g].y), s[4 * g + 1].x, s[4 * g + 1].y);
-                            x = max3(max3(x, s[4 * g + 2].x, s[4 * g + 2].y), s[4 * g + 3].x, s[4 * g + 3].y);
-                            if (x != -INFINITY && plain) x *= sh.ks8[slot][g];
-                            top4[g & 3] = fmaxf(top4[g & 3], x);
-                        }
-                    }
-                };
-                half_done(0);
-                tc_wait_ld();
-                half_done(32);
                 if (edge) {
                     const uint32_t vu = 2u * (n + t) + 1u;
                     mbar_wait(smem_addr(&sh.full[vu % C::STAGES]), (vu / C::STAGES) & 1u, abort_flag, R.error, 0x823u, R.wait_limit_ns);
                     clean_values<FP8, DP>(w, smem_ptr + C::KV_OFF + (vu % C::STAGES) * C::TILE_BYTES, tok0, w.lo, w.hi, r);
                 }
-                const float top = fmaxf(fmaxf(top4[0], top4[1]), fmaxf(top4[2], top4[3]));
-                const float x = top * mul;
-                if (t == 0) {
-                    m = top == -INFINITY ? -INFINITY : x;
-                } else if (__any_sync(0xffffffffu, x > m + C::kRise || (FP8 && down_v != 1.f))) {
-                    const float nm = top == -INFINITY ? m : fmaxf(m, x);
-                    const float f = nm == m ? 1.f : fast_exp2(m - nm);
-                    m = nm;
-                    sum[0] = mul2(sum[0], make_float2(f, f));
-                    sum[1] = mul2(sum[1], make_float2(f, f));
-                    const float g = f * down_v;
-                    uint32_t o[16];
-#pragma unroll 1
-                    for (int c = 0; c < DP / 16; ++c) {
-                        tc_ld16(o, o_at + 16u * c);
-                        tc_wait_ld();
-#pragma unroll
-                        for (int e = 0; e < 16; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * g);
-                        tc_st16(o_at + 16u * c, o);
-                    }
-                }
-                const float ref = m == -INFINITY ? 0.f : -m;
-                const float2 ref_2 = make_float2(ref, ref);
-#pragma unroll
-                for (int c4 = 0; c4 < 4; ++c4) {
-                    uint32_t pk[16];
-                    float2 mul_2 = make_float2(mul, mul);
-#pragma unroll
-                    for (int c = 0; c < 16; ++c) {
-                        if (FP8 && (c & 3) == 0) {
-                            const float f = plain ? fmaxf(mul * sh.ks8[slot][4 * c4 + c / 4], 1e-37f) : mul;   // 0 * -infinity: none
-                            mul_2 = make_float2(f, f);
-                        }
-                        float2 e = fma2(s[16 * c4 + c], mul_2, ref_2);
-                        e.x = fast_exp2(e.x);
-                        e.y = fast_exp2(e.y);
-                        sum[c & 1] = add2(sum[c & 1], e);
-                        if (FP8) {
-                            float2 y;
-                            if (plain) {
-                                const float f = sh.vs8[slot][4 * c4 + c / 4];
-                                y = mul2(e, make_float2(f, f));
-                            } else {
-                                y = mul2(e, reinterpret_cast<const float2 *>(sh.vs[slot])[16 * c4 + c]);
-                                if (e.x == 0.f) y.x = 0.f;   // a masked token stays 0 whatever its scale is
-                                if (e.y == 0.f) y.y = 0.f;
-                            }
-                            pk[c] = f16x2(y.x, y.y);
-                        } else {
-                            pk[c] = bf16x2(e.x, e.y);
-                        }
-                    }
-                    tc_st16(s_at + 16u * c4, pk);
-                    if (c4 & 1) {
-                        tc_wait_st();
-                        tc_fence_before();
-                        __syncwarp();
-                        if (lane == 0) mbar_arrive(smem_addr(c4 == 1 ? &sh.p_half[i] : &sh.p_full[i]));
-                    }
-                }
+                ok = mbar_wait(smem_addr(&sh.s_full[i]), s_phase & 1u, abort_flag, R.error, 0x821u, R.wait_limit_ns);
+                ++s_phase;
+                ok = __all_sync(0xffffffffu, ok);
+                if (!ok) break;
+                tc_fence_after();
+                const uint32_t hb = smem_addr(&sh.p_half[i]), fb = smem_addr(&sh.p_full[i]);
+                if (!FP8 || plain) soft_tile<FP8, true, DP>(sh, S, s_at, o_at, slot, tok0, edge, t == 0, down_v, scales, hb, fb, lane);
+                else soft_tile<FP8, false, DP>(sh, S, s_at, o_at, slot, tok0, edge, t == 0, down_v, scales, hb, fb, lane);
             }
-            l = (sum[0].x + sum[0].y) + (sum[1].x + sum[1].y);
         }
+        const float m = S.m;
+        float l = (S.sum[0].x + S.sum[0].y) + (S.sum[1].x + S.sum[1].y);
         // the next part's queries go in while this one's last products run
         more = next_part(part_no + 1u);
         if (more) next_mul = queries(sh.part[(part_no + 1u) % kRowsParts]);
@@ -1092,11 +1206,11 @@ __device__ __forceinline__ void rows_softmax(const RowsParams &R, RowsShared &sh
                 __syncwarp();
                 tc_ld32(reinterpret_cast<uint32_t *>(o), o_at + 32u * c);
                 tc_wait_ld();
-                if (!live) continue;
-                if (bad_lo < bad_hi) add_not_finite<FP8>(P, w, max(bad_lo, lo), min(bad_hi, hi), 32 * c, o);
+                if (bad_lo < bad_hi && live) add_not_finite<FP8>(P, w, max(bad_lo, S.lo), min(bad_hi, S.hi), 32 * c, o);
                 if (w.whole) {
-                    store_row(P, out, 32 * c, o, inv);
-                } else {
+                    __syncwarp();
+                    store_rows(P, out, live, 32 * c, o, inv, lane);
+                } else if (live) {
 #pragma unroll
                     for (int e = 0; e < 32; e += 4)
                         *reinterpret_cast<float4 *>(part + (size_t)((32 * c + e) / 4 * kRowsBlock + prow) * 4) =
@@ -1128,16 +1242,17 @@ __device__ __forceinline__ void rows_softmax(const RowsParams &R, RowsShared &sh
                     if (seen == others) *counter = 0u;  // ready for the next call
                 }
                 named_sync(3 + i, 128);
-                if (sh.last[i] && live) {
+                if (sh.last[i]) {
                     __threadfence();
                     float jm, jl;
 #pragma unroll 1
                     for (int d = 0; d < (int)P.cache.D; d += 32) {
                         float v[32];
-                        join_row<DP>(P.parts, w.c0, w.c1, prow, d, v, jm, jl);
-                        store_row(P, out, d, v, jl == 0.f ? 0.f : 1.f / jl);
+                        join_row<DP>(P.parts, w.c0, w.c1, live ? prow : 0, d, v, jm, jl);
+                        __syncwarp();
+                        store_rows(P, out, live, d, v, jl == 0.f ? 0.f : 1.f / jl, lane);
                     }
-                    if (P.lse) P.lse[lse_at] = lse_of(jm, jl);
+                    if (P.lse && live) P.lse[lse_at] = lse_of(jm, jl);
                 }
             }
         }
@@ -1158,13 +1273,14 @@ __global__ void __launch_bounds__(128) join_rows_kernel(const __grid_constant__ 
     if (j.parts == 0 || d >= (int)P.cache.D) return;
     const RowsSeq w = rows_seq(P, j.s);
     const int row = j.blk * kRowsBlock + prow;
-    if (row >= w.q_len * (int)P.G) return;
+    const bool live = row < w.q_len * (int)P.G;
+    if (!__any_sync(0xffffffffu, live)) return;
     float v[32], m, l;
-    join_row<DP>(P.parts, blockIdx.x, blockIdx.x + j.parts - 1u, prow, d, v, m, l);
+    join_row<DP>(P.parts, blockIdx.x, blockIdx.x + j.parts - 1u, live ? prow : 0, d, v, m, l);
     uint64_t lse_at;
-    __nv_bfloat16 *out = row_out(P, w.q0, j.h, row, lse_at);
-    store_row(P, out, d, v, l == 0.f ? 0.f : 1.f / l);
-    if (P.lse && d == 0) P.lse[lse_at] = lse_of(m, l);
+    __nv_bfloat16 *out = row_out(P, w.q0, j.h, live ? row : 0, lse_at);
+    store_rows(P, out, live, d, v, l == 0.f ? 0.f : 1.f / l, threadIdx.x & 31);
+    if (P.lse && d == 0 && live) P.lse[lse_at] = lse_of(m, l);
 }
 
 template <bool FP8, int DP>
