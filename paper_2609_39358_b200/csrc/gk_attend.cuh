@@ -13,13 +13,24 @@
 // item: the parts then go to the workspace, and the CTA that delivers an item's last part joins them in
 // the order of the line.
 //
-// A warp works alone: its own ring of stages filled by its own 16-byte asynchronous copies, its own
-// running maximum, sum and output; warps meet only at the end of an item.
+// A warp works alone: its own ring of stages filled by its own copies, its own running maximum, sum and output;
+// warps meet only at the end of an item.  Copies are tensor copies (TMA), one per page and 128 bytes of a row; where
+// pages do not tile a stage, or rows are not 64 or 128 values, 16-byte asynchronous copies row by row.
 #pragma once
 
+#include <cuda.h>  // CUtensorMap
+
+#include "gk_device.cuh"
 #include "gk_seq.cuh"
 
 namespace gk {
+
+// The layer's K and V as a tensor: dimension, token and head (as they lie), page, K or V.
+struct MapDev {
+    CUtensorMap map;
+    uint32_t head_first;  // the second dimension is the head
+    uint32_t rows;        // tokens of a page that one copy takes
+};
 
 struct AttendParams {
     SeqsDev seqs;
@@ -39,20 +50,28 @@ struct AttendParams {
 
 constexpr int kAttendWarps = 4;
 constexpr int kAttendThreads = 32 * kAttendWarps;
-constexpr int kAttendStages = 3;
 constexpr int kAttendRows = 16;
 
-template <bool FP8, int DP>
+#ifndef GK_ATTEND_STAGES
+#define GK_ATTEND_STAGES 3
+#endif
+#ifndef GK_ATTEND_CTAS
+#define GK_ATTEND_CTAS 2
+#endif
+
+template <bool FP8, int DP, bool TMA>
 struct AttendCfg {
+    static constexpr int STAGES = TMA ? GK_ATTEND_STAGES : 3;
+    static constexpr int CTAS = TMA ? GK_ATTEND_CTAS : DP <= 128 ? 2 : 1;   // per SM
     static constexpr int E = FP8 ? 1 : 2;
     static constexpr int TK = FP8 ? 32 : 16;         // tokens of a stage
     static constexpr int TILE = kAttendWarps * TK;   // tokens of a tile
     static constexpr int CPR = DP * E / 16;          // 16-byte pieces of a row
     static constexpr int KV_BYTES = TK * DP * E;
-    static constexpr int SCALE_BYTES = FP8 ? 2 * TK * 4 : 0;
-    static constexpr int STAGE_BYTES = 2 * KV_BYTES + SCALE_BYTES;
+    static constexpr int SCALE_BYTES = FP8 ? 2 * TK * 4 : 0;   // behind the stages
+    static constexpr int STAGE_BYTES = 2 * KV_BYTES;
     static constexpr int PART_FLOATS = kAttendRows * DP + 2 * kAttendRows;  // outputs, maxima, sums
-    static constexpr int SMEM = kAttendWarps * kAttendStages * STAGE_BYTES;
+    static constexpr int SMEM = kAttendWarps * STAGES * (STAGE_BYTES + SCALE_BYTES) + (TMA ? 1024 : 0);
     static_assert(STAGE_BYTES >= kAttendRows * DP * 4, "a stage also holds a warp's output at an item's end");
 };
 
@@ -91,14 +110,16 @@ template <bool F16>
 __device__ __forceinline__ void mma16816(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1)
 {
     if (F16)
-        asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+        asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
                      : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
                      : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
     else
-        asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+        asm("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
                      : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
                      : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
 }
+
+__device__ __forceinline__ void fence_async_smem() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
 
 __device__ __forceinline__ float fast_exp2(float x)
 {
@@ -117,21 +138,30 @@ __device__ __forceinline__ uint32_t f16x2(float lo, float hi)
     const __half2 b = __floats2half2_rn(lo, hi);
     return *reinterpret_cast<const uint32_t *>(&b);
 }
-// two e4m3 values (the low half of w) as f16, exactly
+// two e4m3 values as f16, exactly: the low half of w, and the high half
 __device__ __forceinline__ uint32_t e4m3_to_f16(uint32_t w)
 {
     uint32_t r;
-    asm("{ .reg .b16 t; cvt.u16.u32 t, %1; cvt.rn.f16x2.e4m3x2 %0, t; }" : "=r"(r) : "r"(w));
+    asm("{ .reg .b16 l, h; mov.b32 {l, h}, %1; cvt.rn.f16x2.e4m3x2 %0, l; }" : "=r"(r) : "r"(w));
+    return r;
+}
+__device__ __forceinline__ uint32_t e4m3_to_f16_high(uint32_t w)
+{
+    uint32_t r;
+    asm("{ .reg .b16 l, h; mov.b32 {l, h}, %1; cvt.rn.f16x2.e4m3x2 %0, h; }" : "=r"(r) : "r"(w));
     return r;
 }
 
-// Where the 16-byte piece c of row r of a tile with CPR pieces per row lies: pieces are exchanged within a row so that
-// the 8 rows of one ldmatrix, and the 4 lanes x 2 rows of one 16-byte read, fall on different banks.
-template <int CPR>
+// Where the 16-byte piece c of row r of a K or V stage lies: pieces are exchanged within a row so that the 8 rows of
+// one ldmatrix fall on different banks.  With tensor copies that is the hardware's swizzle (of 128 bytes, rows of
+// 256 bytes in two halves; of 64 for rows of 64).
+template <bool FP8, int DP, bool TMA>
 __device__ __forceinline__ uint32_t piece(uint32_t r, uint32_t c)
 {
-    if (CPR >= 8) return (r * CPR + (c ^ (((r & 1u) << 2) | ((r >> 1) & 3u)))) * 16u;
-    return (r * CPR + (c ^ ((r >> 1) & 3u))) * 16u;
+    using C = AttendCfg<FP8, DP, TMA>;
+    if (C::CPR == 4) return (r * 4u + (c ^ ((r >> 1) & 3u))) * 16u;
+    if (TMA) return (c >> 3) * (C::TK * 128u) + r * 128u + (((c & 7u) ^ (r & 7u)) << 4);
+    return (r * C::CPR + (c ^ (((r & 1u) << 2) | ((r >> 1) & 3u)))) * 16u;
 }
 
 // A sequence as this kernel walks it.
@@ -139,7 +169,7 @@ struct SeqWork {
     int q0, q_len, kv;  // rows, tokens
     int first;          // first token of the first tile
     int tiles;          // tiles of every item of the sequence
-    int items;          // 16-row blocks x key heads
+    int blocks;         // of 16 rows
     bool bad;           // longer than its page table
 };
 
@@ -152,7 +182,7 @@ __device__ __forceinline__ SeqWork seq_work(const AttendParams &P, uint32_t s)
     w.q_len = sp.q_len;
     w.kv = sp.kv;
     w.bad = (uint64_t)sp.kv > (uint64_t)P.seqs.max_pages * P.cache.T;
-    w.items = (int)(((uint32_t)sp.q_len * P.G + (kAttendRows - 1)) / kAttendRows * P.cache.H);
+    w.blocks = (int)(((uint32_t)sp.q_len * P.G + (kAttendRows - 1)) / kAttendRows);
     int lo = 0;
     if (P.window) lo = (int)max(0ll, (long long)sp.kv - sp.q_len + 1 - (long long)P.window);
     w.first = lo / TILE * TILE;
@@ -160,39 +190,24 @@ __device__ __forceinline__ SeqWork seq_work(const AttendParams &P, uint32_t s)
     return w;
 }
 
-// A place in the line of tiles.
-struct TilePos {
-    uint32_t s;
-    int item, tile;
-    SeqWork w;
-};
+// An item counts for its tiles and one more, which comes first: its queries, and joining its warps, take about as long.
+constexpr int kAttendCost = 1;
 
-template <int TILE>
-__device__ __forceinline__ void next_tile(const AttendParams &P, TilePos &c)
+__device__ __forceinline__ long long seq_units(const AttendParams &P, const SeqWork &w)
 {
-    if (++c.tile < c.w.tiles) return;
-    c.tile = 0;
-    if (++c.item < c.w.items) return;
-    c.item = 0;
-    do {
-        if (++c.s >= P.seqs.n_seqs) return;
-        c.w = seq_work<TILE>(P, c.s);
-    } while (c.w.items == 0);
+    return (long long)w.blocks * P.cache.H * (w.tiles + kAttendCost);
 }
 
-// Rows of a 16-row block and the tokens that any of them attends to.
+// Rows of a 16-row block and the tokens that they attend to.
 struct BlockSpan {
     int row0;    // first row (token * G + head of the group)
-    int h;       // key head
     int lo, hi;  // tokens that some row of the block attends to
-    bool mixed;  // its rows do not all attend to the same tokens
+    int all_lo, all_hi;  // tokens that every row attends to
 };
 
-__device__ __forceinline__ BlockSpan block_span(const AttendParams &P, const SeqWork &w, int item)
+__device__ __forceinline__ BlockSpan block_span(const AttendParams &P, const SeqWork &w, int blk)
 {
     BlockSpan b;
-    const int blk = item / (int)P.cache.H;
-    b.h = item - blk * (int)P.cache.H;
     b.row0 = blk * kAttendRows;
     const int rows = w.q_len * (int)P.G;
     const int j0 = (int)P.by_G.div((uint32_t)b.row0);
@@ -200,58 +215,112 @@ __device__ __forceinline__ BlockSpan block_span(const AttendParams &P, const Seq
     const int at = w.kv - w.q_len;
     b.hi = P.causal ? max(0, at + j1 + 1) : w.kv;
     b.lo = P.window ? (int)max(0ll, (long long)at + j0 + 1 - (long long)P.window) : 0;
-    b.mixed = j0 != j1 && (P.causal || P.window);
+    b.all_hi = P.causal ? max(0, at + j0 + 1) : w.kv;
+    b.all_lo = P.window ? (int)max(0ll, (long long)at + j1 + 1 - (long long)P.window) : 0;
     return b;
 }
 
-// What a lane knows about "its" token of the next stage to be loaded.
-struct TokenMeta {
-    int64_t at;       // byte offset of the token's row from the layer's k or v, or -1: no token here
-    uint32_t s_at;    // unused without scales
-    bool bad;         // a page id that the table should have held is missing
+// A place in the line of tiles.
+struct TilePos {
+    uint32_t s;
+    SeqWork w;
+    int blk, h, tile;
+    int unit;        // from the beginning of the stretch
+    BlockSpan b;
 };
 
-template <bool FP8, int DP>
-__device__ __forceinline__ TokenMeta token_meta(const AttendParams &P, const TilePos &c, int warp, int lane)
+template <int TILE>
+__device__ __forceinline__ void next_tile(const AttendParams &P, TilePos &c)
 {
-    using C = AttendCfg<FP8, DP>;
-    TokenMeta m{-1, 0, c.w.bad};
-    const int tok = c.w.first + c.tile * C::TILE + warp * C::TK + lane;
-    const BlockSpan b = block_span(P, c.w, c.item);
-    if (lane < C::TK && tok >= b.lo && tok < b.hi && !c.w.bad) {
+    ++c.unit;
+    if (++c.tile < c.w.tiles) return;
+    c.tile = 0;
+    c.unit += kAttendCost;
+    if (++c.h < (int)P.cache.H) return;
+    c.h = 0;
+    if (++c.blk >= c.w.blocks) {
+        c.blk = 0;
+        do {
+            if (++c.s >= P.seqs.n_seqs) return;
+            c.w = seq_work<TILE>(P, c.s);
+        } while (c.w.blocks == 0);
+    }
+    c.b = block_span(P, c.w, c.blk);
+}
+
+// What a lane knows about "its" token of the next stage to be loaded.  The page id is not looked at before the stage
+// is issued: that would wait for its load.
+struct TokenMeta {
+    int page;    // as the table has it
+    int row;     // in the page
+    bool want;   // there is a token to be loaded
+};
+
+template <bool FP8, int DP, bool TMA>
+__device__ __forceinline__ TokenMeta token_meta(const AttendParams &P, uint32_t map_rows, const TilePos &c, int warp, int lane)
+{
+    using C = AttendCfg<FP8, DP, TMA>;
+    TokenMeta m{-1, 0, false};
+    const int tok0 = c.w.first + c.tile * C::TILE + warp * C::TK, tok = tok0 + lane;
+    m.want = lane < C::TK && tok >= c.b.lo && tok < c.b.hi;
+    if (TMA) {   // the whole of a page's part is copied, or none of it
+        const int from = tok0 + (lane & ~((int)map_rows - 1));
+        m.want = lane < C::TK && from < c.b.hi && from + (int)map_rows > c.b.lo;
+    }
+    if (m.want && !c.w.bad) {
         const uint32_t page = P.cache.by_T.div((uint32_t)tok);
-        const int g = __ldg(P.seqs.page_table + (uint64_t)c.s * P.seqs.table_stride + page);
-        if ((uint32_t)g < P.cache.num_pages) {
-            m.at = (int64_t)((uint64_t)g * P.cache.page + (uint64_t)((uint32_t)tok - page * P.cache.T) * P.cache.tok +
-                             (uint64_t)b.h * P.cache.head);
-            m.s_at = (uint32_t)g;
-        } else {
-            m.bad = true;
-        }
+        m.page = __ldg(P.seqs.page_table + (uint64_t)c.s * P.seqs.table_stride + page);
+        m.row = tok - (int)(page * P.cache.T);
     }
     return m;
 }
 
-template <bool FP8, int DP>
-__device__ __forceinline__ void load_stage(const AttendParams &P, uint32_t stage, const TokenMeta &m, int h, int lane)
+// Returns whether a page that the table should have held is missing.
+template <bool FP8, int DP, bool TMA>
+__device__ __forceinline__ bool load_stage(const AttendParams &P, const MapDev &M, uint32_t stage, uint32_t scales, uint32_t bar,
+                                           const TokenMeta &m, int h, int lane)
 {
-    using C = AttendCfg<FP8, DP>;
-    const uint32_t pieces = P.cache.D * C::E / 16u;
+    using C = AttendCfg<FP8, DP, TMA>;
+    const bool have = m.want && (uint32_t)m.page < P.cache.num_pages;
+    if (TMA) {
+        const bool lead = have && ((uint32_t)lane & (M.rows - 1u)) == 0u;
+        const uint32_t copies = (uint32_t)__popc(__ballot_sync(0xffffffffu, lead));
+        if (lane == 0) mbar_arrive_expect_tx(bar, copies * M.rows * DP * C::E * 2u);
+        __syncwarp();
+        if (lead) {
+            constexpr int PIECES = DP * C::E > 128 ? DP * C::E / 128 : 1;
+            constexpr uint32_t ROW = DP * C::E > 128 ? 128u : DP * C::E;
 #pragma unroll
-    for (int i = 0; i < C::TK * C::CPR / 32; ++i) {
-        const uint32_t j = (uint32_t)lane + 32u * i, r = j / C::CPR, c = j % C::CPR;
-        const int64_t at = __shfl_sync(0xffffffffu, m.at, (int)r);
-        const bool take = at >= 0 && c < pieces;
-        const uint64_t off = take ? (uint64_t)at + 16u * c : 0u;
-        const uint32_t d = stage + piece<C::CPR>(r, c);
-        copy16(d, P.cache.k + off, take);
-        copy16(d + C::KV_BYTES, P.cache.v + off, take);
+            for (int kv = 0; kv < 2; ++kv)
+#pragma unroll
+                for (int p = 0; p < PIECES; ++p)
+                    asm volatile("cp.async.bulk.tensor.5d.shared::cta.global.tile.mbarrier::complete_tx::bytes [%0], "
+                                 "[%1, {%2, %3, %4, %5, %6}], [%7];" ::"r"(stage + kv * C::KV_BYTES + p * C::TK * 128 + lane * ROW),
+                                 "l"(&M.map), "r"(64 * p), "r"(M.head_first ? h : m.row), "r"(M.head_first ? m.row : h), "r"(m.page),
+                                 "r"(kv), "r"(bar)
+                                 : "memory");
+        }
+    } else {
+        const uint32_t pieces = P.cache.D * C::E / 16u;
+        const int64_t at = !have ? -1 : (int64_t)((uint64_t)m.page * P.cache.page + (uint64_t)m.row * P.cache.tok +
+                                                      (uint64_t)h * P.cache.head);
+#pragma unroll
+        for (int i = 0; i < C::TK * C::CPR / 32; ++i) {
+            const uint32_t j = (uint32_t)lane + 32u * i, r = j / C::CPR, c = j % C::CPR;
+            const int64_t of_row = __shfl_sync(0xffffffffu, at, (int)r);
+            const bool take = of_row >= 0 && c < pieces;
+            const uint64_t off = take ? (uint64_t)of_row + 16u * c : 0u;
+            const uint32_t d = stage + piece<FP8, DP, TMA>(r, c);
+            copy16(d, P.cache.k + off, take);
+            copy16(d + C::KV_BYTES, P.cache.v + off, take);
+        }
     }
     if (FP8 && lane < C::TK) {
-        const uint64_t off = m.at >= 0 ? (uint64_t)m.s_at * P.cache.s_page + (uint32_t)h : 0u;
-        copy4(stage + 2 * C::KV_BYTES + 4 * lane, P.cache.ks + off, m.at >= 0);
-        copy4(stage + 2 * C::KV_BYTES + 4 * (C::TK + lane), P.cache.vs + off, m.at >= 0);
+        const uint64_t off = have ? (uint64_t)m.page * P.cache.s_page + (uint32_t)h : 0u;
+        copy4(scales + 4 * lane, P.cache.ks + off, have);
+        copy4(scales + 4 * (C::TK + lane), P.cache.vs + off, have);
     }
+    return __any_sync(0xffffffffu, m.want && !have);
 }
 
 // Rows g and g + 8 of a 16-row block, as a lane sees them.
@@ -261,7 +330,7 @@ struct LaneRows {
 };
 
 template <bool FP8, int DP>
-__device__ __forceinline__ void load_queries(const AttendParams &P, const SeqWork &w, const BlockSpan &b, int lane,
+__device__ __forceinline__ void load_queries(const AttendParams &P, const SeqWork &w, const BlockSpan &b, int h, int lane,
                                              uint32_t (&qa)[DP / 16][4], LaneRows &lr)
 {
     const int g = lane >> 2, t = lane & 3;
@@ -272,7 +341,7 @@ __device__ __forceinline__ void load_queries(const AttendParams &P, const SeqWor
         const int r = b.row0 + g + 8 * half;
         const bool live = r < rows;
         const uint32_t j = P.by_G.div((uint32_t)(live ? r : 0));
-        const uint32_t head = (uint32_t)b.h * P.G + (uint32_t)((live ? r : 0) - (int)(j * P.G));
+        const uint32_t head = (uint32_t)h * P.G + (uint32_t)((live ? r : 0) - (int)(j * P.G));
         const __nv_bfloat16 *p = P.q + (uint64_t)(w.q0 + j) * P.q_tok + (uint64_t)head * P.q_head;
         const int pos = at + (int)j;
         lr.hi[half] = !live ? 0 : P.causal ? max(0, pos + 1) : w.kv;
@@ -344,10 +413,10 @@ __device__ __forceinline__ int out_dim(int n, int e, int t)
 }
 
 // Does a stage's V hold an infinity or NaN?
-template <bool FP8, int DP>
+template <bool FP8, int DP, bool TMA>
 __device__ __forceinline__ bool values_not_finite(const uint8_t *v, int lane)
 {
-    using C = AttendCfg<FP8, DP>;
+    using C = AttendCfg<FP8, DP, TMA>;
     bool found = false;
     for (int i = lane; i < C::KV_BYTES / 4; i += 32) {
         const uint32_t w = *reinterpret_cast<const uint32_t *>(v + 4 * i);
@@ -357,11 +426,11 @@ __device__ __forceinline__ bool values_not_finite(const uint8_t *v, int lane)
     return __any_sync(0xffffffffu, found);
 }
 
-template <bool FP8, int DP>
-__device__ __forceinline__ void add_values_by_element(const uint8_t *v, const float (&s)[AttendCfg<FP8, DP>::TK / 8][4],
+template <bool FP8, int DP, bool TMA>
+__device__ __forceinline__ void add_values_by_element(const uint8_t *v, const float (&s)[AttendCfg<FP8, DP, TMA>::TK / 8][4],
                                                       Running<DP> &R, int lane)
 {
-    using C = AttendCfg<FP8, DP>;
+    using C = AttendCfg<FP8, DP, TMA>;
     const int t = lane & 3;
 #pragma unroll
     for (int n8 = 0; n8 < C::TK / 8; ++n8)
@@ -376,7 +445,7 @@ __device__ __forceinline__ void add_values_by_element(const uint8_t *v, const fl
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
                     const int d = out_dim<FP8>(n, e, t) * C::E;
-                    const uint8_t *p = v + piece<C::CPR>(8 * n8 + k, d / 16) + d % 16;
+                    const uint8_t *p = v + piece<FP8, DP, TMA>(8 * n8 + k, d / 16) + d % 16;
                     float x;
                     if (FP8) x = __half2float(__half(__nv_cvt_fp8_to_halfraw(*p, __NV_E4M3)));
                     else x = __bfloat162float(*reinterpret_cast<const __nv_bfloat16 *>(p));
@@ -385,67 +454,84 @@ __device__ __forceinline__ void add_values_by_element(const uint8_t *v, const fl
         }
 }
 
-template <bool FP8, int DP>
-__device__ __forceinline__ void attend_stage(const AttendParams &P, uint32_t stage, const uint8_t *stage_ptr, int tok0,
-                                             const uint32_t (&qa)[DP / 16][4], const LaneRows &lr, Running<DP> &R, bool mixed, int lane)
+template <bool FP8, int DP, bool TMA>
+__device__ __forceinline__ void attend_stage(const AttendParams &P, uint32_t stage, const uint8_t *stage_ptr, const float *scales, int tok0,
+                                             const uint32_t (&qa)[DP / 16][4], const LaneRows &lr, Running<DP> &R, bool partial, int blo, int bhi, int lane)
 {
-    using C = AttendCfg<FP8, DP>;
+    using C = AttendCfg<FP8, DP, TMA>;
     const int t = lane & 3;
     float s[C::TK / 8][4];
 #pragma unroll
     for (int n = 0; n < C::TK / 8; ++n)
 #pragma unroll
         for (int e = 0; e < 4; ++e) s[n][e] = 0.f;
-    // scores
+    // scores: operands of all tokens first, then the tiles of 8 tokens in turn, so that no product waits for the last one
+    if (!FP8) {
 #pragma unroll
-    for (int n = 0; n < C::TK / 8; ++n) {
-        if (!FP8) {
-            const uint32_t r = 8u * n + (lane & 7);
+        for (int k = 0; k < DP / 32; k += 2) {
+            uint32_t b[2][C::TK / 8][4];
 #pragma unroll
-            for (int k = 0; k < DP / 32; ++k) {
-                uint32_t b[4];
-                ldmatrix4(b, stage + piece<C::CPR>(r, 4u * k + (lane >> 3)));
-                mma16816<false>(s[n], qa[2 * k], b[0], b[1]);
-                mma16816<false>(s[n], qa[2 * k + 1], b[2], b[3]);
-            }
-        } else {
-            const uint32_t r = 8u * n + (lane >> 2);
+            for (int j = 0; j < 2; ++j)
 #pragma unroll
-            for (int j = 0; j < DP / 64; ++j) {
-                const uint4 u = *reinterpret_cast<const uint4 *>(stage_ptr + piece<C::CPR>(r, 4u * j + t));
-                const uint32_t w[4] = {u.x, u.y, u.z, u.w};
+                for (int n = 0; n < C::TK / 8; ++n)
+                    ldmatrix4(b[j][n], stage + piece<FP8, DP, TMA>(8u * n + (lane & 7), 4u * (k + j) + (lane >> 3)));
 #pragma unroll
-                for (int k = 0; k < 4; ++k)
-                    mma16816<true>(s[n], qa[4 * j + k], e4m3_to_f16(w[k]), e4m3_to_f16(w[k] >> 16));
-            }
+            for (int j = 0; j < 4; ++j)
+#pragma unroll
+                for (int n = 0; n < C::TK / 8; ++n)
+                    mma16816<false>(s[n], qa[2 * k + j], b[j >> 1][n][2 * (j & 1)], b[j >> 1][n][2 * (j & 1) + 1]);
+        }
+    } else {
+#pragma unroll
+        for (int j = 0; j < DP / 64; ++j) {
+            uint4 u[C::TK / 8];
+#pragma unroll
+            for (int n = 0; n < C::TK / 8; ++n)
+                u[n] = *reinterpret_cast<const uint4 *>(stage_ptr + piece<FP8, DP, TMA>(8u * n + (lane >> 2), 4u * j + t));
+#pragma unroll
+            for (int k = 0; k < 4; ++k)
+#pragma unroll
+                for (int n = 0; n < C::TK / 8; ++n) {
+                    const uint32_t w = k == 0 ? u[n].x : k == 1 ? u[n].y : k == 2 ? u[n].z : u[n].w;
+                    mma16816<true>(s[n], qa[4 * j + k], e4m3_to_f16(w), e4m3_to_f16_high(w));
+                }
         }
     }
     // scale, mask, running maximum
-    const float *scales = reinterpret_cast<const float *>(stage_ptr + 2 * C::KV_BYTES);
     float top[2] = {-INFINITY, -INFINITY};
 #pragma unroll
     for (int n = 0; n < C::TK / 8; ++n) {
-        float ks[2] = {1.f, 1.f};
         if (FP8) {
             const float2 f = *reinterpret_cast<const float2 *>(scales + 8 * n + 2 * t);
-            ks[0] = f.x;
-            ks[1] = f.y;
+            s[n][0] *= f.x * lr.mul[0];
+            s[n][1] *= f.y * lr.mul[0];
+            s[n][2] *= f.x * lr.mul[1];
+            s[n][3] *= f.y * lr.mul[1];
+        } else {
+#pragma unroll
+            for (int e = 0; e < 4; ++e) s[n][e] *= lr.mul[e >> 1];
+        }
+        if (partial) {
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const int tok = tok0 + 8 * n + 2 * t + (e & 1);
+                if (tok < lr.lo[e >> 1] || tok >= lr.hi[e >> 1]) s[n][e] = -INFINITY;
+            }
         }
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-            const int half = e >> 1, tok = tok0 + 8 * n + 2 * t + (e & 1);
-            float x = s[n][e] * lr.mul[half];
-            if (FP8) x *= ks[e & 1];
-            if (tok < lr.lo[half] || tok >= lr.hi[half]) x = -INFINITY;
-            s[n][e] = x;
-            top[half] = fmaxf(top[half], x);
-        }
+        for (int half = 0; half < 2; ++half) top[half] = fmaxf(top[half], fmaxf(s[n][2 * half], s[n][2 * half + 1]));
     }
     float vtop = 0.f;
+    bool odd = false;   // a value scale that is no number: it may reach only what attends to its tokens
     if (FP8) {
         vtop = lane < C::TK ? fabsf(scales[C::TK + lane]) : 0.f;
-        if (!(vtop <= 3.402823466e38f)) vtop = 0.f;  // a scale that is no number counts only where it is used
         vtop = __uint_as_float(__reduce_max_sync(0xffffffffu, __float_as_uint(vtop)));
+        if (!(vtop <= 3.402823466e38f)) {
+            odd = true;
+            vtop = lane < C::TK ? fabsf(scales[C::TK + lane]) : 0.f;
+            if (!(vtop <= 3.402823466e38f)) vtop = 0.f;
+            vtop = __uint_as_float(__reduce_max_sync(0xffffffffu, __float_as_uint(vtop)));
+        }
     }
     bool rise = FP8 && vtop > R.vref;
 #pragma unroll
@@ -488,18 +574,34 @@ __device__ __forceinline__ void attend_stage(const AttendParams &P, uint32_t sta
         for (int n = 0; n < C::TK / 8; ++n) {
             const float2 f = *reinterpret_cast<const float2 *>(scales + C::TK + 8 * n + 2 * t);
             const float v0 = f.x * up, v1 = f.y * up;
-            // a token that a row does not attend to stays 0 whatever its scale is
-            s[n][0] = s[n][0] == 0.f ? 0.f : s[n][0] * v0;
-            s[n][1] = s[n][1] == 0.f ? 0.f : s[n][1] * v1;
-            s[n][2] = s[n][2] == 0.f ? 0.f : s[n][2] * v0;
-            s[n][3] = s[n][3] == 0.f ? 0.f : s[n][3] * v1;
+            const float z[4] = {s[n][0], s[n][1], s[n][2], s[n][3]};
+            s[n][0] *= v0;
+            s[n][1] *= v1;
+            s[n][2] *= v0;
+            s[n][3] *= v1;
+            if (odd) {
+#pragma unroll
+                for (int e = 0; e < 4; ++e)
+                    if (z[e] == 0.f) s[n][e] = 0.f;
+            }
         }
     }
     // outputs
     const uint32_t vbase = stage + C::KV_BYTES;
-    if (mixed && values_not_finite<FP8, DP>(stage_ptr + C::KV_BYTES, lane)) {
+    if (TMA && partial) {
+        // what no row of the block attends to -- the rest of a page, or whatever was in a stage that was not filled -- counts as 0
+        for (int i = lane; i < C::TK * C::CPR; i += 32) {
+            const int r = i / C::CPR;
+            if (tok0 + r < blo || tok0 + r >= bhi)
+                *reinterpret_cast<uint4 *>(const_cast<uint8_t *>(stage_ptr) + C::KV_BYTES + piece<FP8, DP, TMA>(r, i % C::CPR)) =
+                    make_uint4(0u, 0u, 0u, 0u);
+        }
+        fence_async_smem();   // the next tensor copy into the stage comes after these
+        __syncwarp();
+    }
+    if (partial && values_not_finite<FP8, DP, TMA>(stage_ptr + C::KV_BYTES, lane)) {
         // 0 * infinity would reach rows that do not attend to the token: element by element, by weight
-        add_values_by_element<FP8, DP>(stage_ptr + C::KV_BYTES, s, R, lane);
+        add_values_by_element<FP8, DP, TMA>(stage_ptr + C::KV_BYTES, s, R, lane);
         return;
     }
 #pragma unroll
@@ -521,10 +623,10 @@ __device__ __forceinline__ void attend_stage(const AttendParams &P, uint32_t sta
 #pragma unroll
             for (int n = 0; n < DP / 16; ++n) {
                 uint32_t b[4];
-                ldmatrix4_trans(b, vbase + piece<C::CPR>(r, 2u * n + (lane >> 4)));
+                ldmatrix4_trans(b, vbase + piece<FP8, DP, TMA>(r, 2u * n + (lane >> 4)));
                 mma16816<false>(R.o[2 * n], hi, b[0], b[1]);
-                mma16816<false>(R.o[2 * n], lo, b[0], b[1]);
                 mma16816<false>(R.o[2 * n + 1], hi, b[2], b[3]);
+                mma16816<false>(R.o[2 * n], lo, b[0], b[1]);
                 mma16816<false>(R.o[2 * n + 1], lo, b[2], b[3]);
             }
         } else {
@@ -536,12 +638,12 @@ __device__ __forceinline__ void attend_stage(const AttendParams &P, uint32_t sta
 #pragma unroll
             for (int n = 0; n < DP / 32; ++n) {
                 uint32_t b[4];
-                ldmatrix4_trans(b, vbase + piece<C::CPR>(r, 2u * n + (lane >> 4)));
+                ldmatrix4_trans(b, vbase + piece<FP8, DP, TMA>(r, 2u * n + (lane >> 4)));
 #pragma unroll
                 for (int e = 0; e < 2; ++e) {
                     const uint32_t x = __byte_perm(b[2 * e], 0, 0x3120), y = __byte_perm(b[2 * e + 1], 0, 0x3120);
                     mma16816<true>(R.o[4 * n + 2 * e], a, e4m3_to_f16(x), e4m3_to_f16(y));
-                    mma16816<true>(R.o[4 * n + 2 * e + 1], a, e4m3_to_f16(x >> 16), e4m3_to_f16(y >> 16));
+                    mma16816<true>(R.o[4 * n + 2 * e + 1], a, e4m3_to_f16_high(x), e4m3_to_f16_high(y));
                 }
             }
         }
@@ -549,131 +651,161 @@ __device__ __forceinline__ void attend_stage(const AttendParams &P, uint32_t sta
 }
 
 template <int DP>
-__device__ __forceinline__ void write_row_piece(const AttendParams &P, const SeqWork &w, const BlockSpan &b, int row, int d,
+__device__ __forceinline__ void write_row_piece(const AttendParams &P, const SeqWork &w, const BlockSpan &b, int h, int row, int d,
                                                 const float4 &v)
 {
     const int r = b.row0 + row;
     const uint32_t j = P.by_G.div((uint32_t)r);
-    const uint32_t head = (uint32_t)b.h * P.G + (uint32_t)(r - (int)(j * P.G));
+    const uint32_t head = (uint32_t)h * P.G + (uint32_t)(r - (int)(j * P.G));
     if (d < (int)P.cache.D)
         *reinterpret_cast<uint2 *>(P.out + (uint64_t)(w.q0 + j) * P.o_tok + (uint64_t)head * P.o_head + d) =
             make_uint2(bf16x2(v.x, v.y), bf16x2(v.z, v.w));
 }
 
-__device__ __forceinline__ void write_lse(const AttendParams &P, const SeqWork &w, const BlockSpan &b, int row, float m, float l)
+__device__ __forceinline__ void write_lse(const AttendParams &P, const SeqWork &w, const BlockSpan &b, int h, int row, float m, float l)
 {
     const int r = b.row0 + row;
     const uint32_t j = P.by_G.div((uint32_t)r);
-    const uint32_t head = (uint32_t)b.h * P.G + (uint32_t)(r - (int)(j * P.G));
+    const uint32_t head = (uint32_t)h * P.G + (uint32_t)(r - (int)(j * P.G));
     if (P.lse) P.lse[(uint64_t)(w.q0 + j) * P.Hq + head] = l == 0.f ? -INFINITY : m * 0.69314718055994531f + logf(l);
 }
 
-template <bool FP8, int DP>
-__global__ void __launch_bounds__(kAttendThreads, DP <= 128 ? 2 : 1) attend_kernel(const AttendParams P)
+template <bool FP8, int DP, bool TMA>
+__global__ void __launch_bounds__(kAttendThreads, AttendCfg<FP8, DP, TMA>::CTAS)
+    attend_kernel(const __grid_constant__ AttendParams P, const __grid_constant__ MapDev M, uint32_t *error, unsigned long long wait_limit_ns)
 {
-    using C = AttendCfg<FP8, DP>;
-    extern __shared__ __align__(128) uint8_t smem[];
+    using C = AttendCfg<FP8, DP, TMA>;
+    extern __shared__ __align__(128) uint8_t smem_raw[];
+    uint8_t *smem = smem_raw + (TMA ? (1024u - (smem_addr(smem_raw) & 1023u)) & 1023u : 0u);
+    __shared__ unsigned long long sh_full[kAttendWarps][C::STAGES];
+    __shared__ uint32_t sh_abort;
     __shared__ long long sh_total[kAttendWarps];
     __shared__ long long sh_at;
     __shared__ uint32_t sh_seq;
     __shared__ float sh_m[kAttendWarps][kAttendRows], sh_l[kAttendWarps][kAttendRows];
     __shared__ uint32_t sh_last;
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+    if (TMA && tid == 0) {
+        for (int i = 0; i < kAttendWarps * C::STAGES; ++i) mbar_init(smem_addr(&sh_full[0][0] + i), 1);
+        sh_abort = 0u;
+        fence_mbar_init();
+    }
 
-    // the length of the line of tiles, and where this CTA's stretch of it begins
-    long long total = 0;
+    // the length of the line, and where this CTA's stretch of it begins; a thread per sequence
+    long long total = 0, mine = 0, upto = 0;   // units of this thread's sequence, and of those up to it among the first
+    SeqWork own;
     for (uint32_t s0 = 0; s0 < P.seqs.n_seqs; s0 += kAttendThreads) {
         long long n = 0;
         if (s0 + tid < P.seqs.n_seqs) {
-            const SeqWork w = seq_work<C::TILE>(P, s0 + tid);
-            n = (long long)w.items * w.tiles;
+            own = seq_work<C::TILE>(P, s0 + tid);
+            n = seq_units(P, own);
         }
+        long long incl = n;
 #pragma unroll
-        for (int o = 16; o; o >>= 1) n += __shfl_xor_sync(0xffffffffu, n, o);
-        if (lane == 0) sh_total[warp] = n;
+        for (int o = 1; o < 32; o <<= 1) {
+            const long long x = __shfl_up_sync(0xffffffffu, incl, o);
+            if (lane >= o) incl += x;
+        }
+        if (s0) __syncthreads();
+        if (lane == 31) sh_total[warp] = incl;
         __syncthreads();
 #pragma unroll
-        for (int i = 0; i < kAttendWarps; ++i) total += sh_total[i];
-        __syncthreads();
+        for (int i = 0; i < kAttendWarps; ++i) {
+            if (i < warp && s0 == 0) upto += sh_total[i];
+            total += sh_total[i];
+        }
+        if (s0 == 0) {
+            upto += incl;
+            mine = n;
+        }
     }
     if (total == 0) return;
     const long long ctas = total < (long long)gridDim.x ? total : (long long)gridDim.x;
     if ((long long)blockIdx.x >= ctas) return;
     const long long begin = total * blockIdx.x / ctas, end = total * (blockIdx.x + 1) / ctas;
-    {
-        long long before = 0;
-        for (uint32_t s0 = 0; s0 < P.seqs.n_seqs; s0 += kAttendThreads) {
-            long long n = 0;
-            if (s0 + tid < P.seqs.n_seqs) {
-                const SeqWork w = seq_work<C::TILE>(P, s0 + tid);
-                n = (long long)w.items * w.tiles;
-            }
-            long long incl = n;
-#pragma unroll
-            for (int o = 1; o < 32; o <<= 1) {
-                const long long x = __shfl_up_sync(0xffffffffu, incl, o);
-                if (lane >= o) incl += x;
-            }
-            if (lane == 31) sh_total[warp] = incl;
-            __syncthreads();
-            long long base = before;
-            for (int i = 0; i < warp; ++i) base += sh_total[i];
-            const long long lo = base + incl - n;
-            if (n > 0 && begin >= lo && begin < lo + n) {
-                sh_seq = s0 + tid;
-                sh_at = lo;
-            }
-            for (int i = 0; i < kAttendWarps; ++i) before += sh_total[i];
-            __syncthreads();
-            if (before > begin) break;
+    for (uint32_t s0 = 0;;) {   // the first sequences are at hand; later ones are looked up again
+        if (mine > 0 && begin >= upto - mine && begin < upto) {
+            sh_seq = s0 + tid;
+            sh_at = upto - mine;
         }
+        if (P.seqs.n_seqs <= kAttendThreads) break;
+        long long last = upto;
+        if (tid == kAttendThreads - 1) sh_total[0] = last;
+        __syncthreads();
+        last = sh_total[0];
+        if (begin < last) break;
+        s0 += kAttendThreads;
+        mine = 0;
+        if (s0 + tid < P.seqs.n_seqs) {
+            const SeqWork w = seq_work<C::TILE>(P, s0 + tid);
+            mine = seq_units(P, w);
+        }
+        upto = mine;
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) {
+            const long long x = __shfl_up_sync(0xffffffffu, upto, o);
+            if (lane >= o) upto += x;
+        }
+        __syncthreads();
+        if (lane == 31) sh_total[warp] = upto;
+        __syncthreads();
+        upto += last;
+        for (int i = 0; i < warp; ++i) upto += sh_total[i];
+        __syncthreads();
     }
+    __syncthreads();
 
     TilePos comp;
     comp.s = sh_seq;
     comp.w = seq_work<C::TILE>(P, comp.s);
     {
         const long long off = begin - sh_at;
-        comp.item = (int)(off / comp.w.tiles);
-        comp.tile = (int)(off - (long long)comp.item * comp.w.tiles);
+        const int per = comp.w.tiles + kAttendCost;
+        const long long item = off / per;
+        const int u = (int)(off - item * per);
+        comp.blk = (int)(item / P.cache.H);
+        comp.h = (int)(item - (long long)comp.blk * P.cache.H);
+        comp.tile = max(0, u - kAttendCost);
+        comp.unit = max(0, kAttendCost - u);
+        comp.b = block_span(P, comp.w, comp.blk);
     }
+    const int units = (int)(end - begin);
+    if (comp.unit >= units) return;   // the stretch is an item's extra unit
     TilePos load = comp;  // runs ahead of comp
-    const int n_tiles = (int)(end - begin);
-    const uint32_t ring = smem_addr(smem) + warp * kAttendStages * C::STAGE_BYTES;
-    const uint8_t *ring_ptr = smem + warp * kAttendStages * C::STAGE_BYTES;
+    const uint32_t ring = smem_addr(smem) + warp * C::STAGES * C::STAGE_BYTES;
+    const uint8_t *ring_ptr = smem + warp * C::STAGES * C::STAGE_BYTES;
+    uint8_t *scale_ptr = smem + kAttendWarps * C::STAGES * C::STAGE_BYTES + warp * C::STAGES * C::SCALE_BYTES;
+    const uint32_t scale_ring = smem_addr(scale_ptr);
+    const uint32_t full0 = smem_addr(&sh_full[warp][0]);
 
-    TokenMeta meta = token_meta<FP8, DP>(P, load, warp, lane);
+    TokenMeta meta = token_meta<FP8, DP, TMA>(P, M.rows, load, warp, lane);
     uint32_t bad_stages = 0;  // bit s: the load in stage s met a missing page
     int loaded = 0;
     auto issue = [&](int stage) {
-        if (loaded < n_tiles) {
-            const int h = load.item % (int)P.cache.H;
-            load_stage<FP8, DP>(P, ring + stage * C::STAGE_BYTES, meta, h, lane);
-            const bool bad = __any_sync(0xffffffffu, meta.bad);
+        if (load.unit < units) {
+            const bool bad = load_stage<FP8, DP, TMA>(P, M, ring + stage * C::STAGE_BYTES, scale_ring + stage * C::SCALE_BYTES,
+                                                      full0 + 8u * stage, meta, load.h, lane);
             bad_stages = (bad_stages & ~(1u << stage)) | ((bad ? 1u : 0u) << stage);
             if (bad && lane == 0 && P.seqs.status) P.seqs.status[load.s] = 2;  // GK_JOB_PAGE_TABLE
-            if (++loaded < n_tiles) {
-                next_tile<C::TILE>(P, load);
-                meta = token_meta<FP8, DP>(P, load, warp, lane);
-            }
+            ++loaded;
+            next_tile<C::TILE>(P, load);
+            if (load.unit < units) meta = token_meta<FP8, DP, TMA>(P, M.rows, load, warp, lane);
         }
-        copy_commit();
+        if (!TMA || FP8) copy_commit();
     };
 #pragma unroll
-    for (int i = 0; i < kAttendStages; ++i) issue(i);
+    for (int i = 0; i < C::STAGES; ++i) issue(i);
 
     uint32_t qa[DP / 16][4];
     LaneRows lr;
     Running<DP> R;
-    BlockSpan b;
     bool fresh = true;
     int stage = 0;
+    uint32_t phase = 0;
     const int g = lane >> 2, t = lane & 3;
-    long long item_first = begin - comp.tile;  // place of the item's first tile in the line
-    for (int n = 0; n < n_tiles; ++n) {
+    while (comp.unit < units) {
         if (fresh) {
-            b = block_span(P, comp.w, comp.item);
-            load_queries<FP8, DP>(P, comp.w, b, lane, qa, lr);
+            load_queries<FP8, DP>(P, comp.w, comp.b, comp.h, lane, qa, lr);
 #pragma unroll
             for (int i = 0; i < DP / 8; ++i)
 #pragma unroll
@@ -683,16 +815,19 @@ __global__ void __launch_bounds__(kAttendThreads, DP <= 128 ? 2 : 1) attend_kern
             R.vref = 0.f;
             fresh = false;
         }
-        copy_wait<kAttendStages - 1>();
+        if (!TMA || FP8) copy_wait<C::STAGES - 1>();
+        if (TMA) mbar_wait(full0 + 8u * stage, phase, &sh_abort, error, 0x841u, wait_limit_ns);
         __syncwarp();
-        attend_stage<FP8, DP>(P, ring + stage * C::STAGE_BYTES, ring_ptr + stage * C::STAGE_BYTES,
-                              comp.w.first + comp.tile * C::TILE + warp * C::TK, qa, lr, R, b.mixed, lane);
+        const int tok0 = comp.w.first + comp.tile * C::TILE + warp * C::TK;
+        attend_stage<FP8, DP, TMA>(P, ring + stage * C::STAGE_BYTES, ring_ptr + stage * C::STAGE_BYTES,
+                                   reinterpret_cast<const float *>(scale_ptr + stage * C::SCALE_BYTES), tok0, qa, lr, R,
+                                   tok0 < comp.b.all_lo || tok0 + C::TK > comp.b.all_hi, comp.b.lo, comp.b.hi, lane);
         if ((bad_stages >> stage) & 1u) R.l[0] = R.l[1] = __int_as_float(0x7fc00000);
         __syncwarp();
         const bool item_ends = comp.tile + 1 == comp.w.tiles;
-        if (item_ends || n + 1 == n_tiles) {
+        if (item_ends || comp.unit + 1 >= units) {
             // the four warps' results meet: each in the stage that it has just used up
-            float *mine = reinterpret_cast<float *>(smem + (warp * kAttendStages + stage) * C::STAGE_BYTES);
+            float *mine = reinterpret_cast<float *>(smem + (warp * C::STAGES + stage) * C::STAGE_BYTES);
 #pragma unroll
             for (int half = 0; half < 2; ++half) {
                 R.l[half] += __shfl_xor_sync(0xffffffffu, R.l[half], 1);
@@ -709,9 +844,10 @@ __global__ void __launch_bounds__(kAttendThreads, DP <= 128 ? 2 : 1) attend_kern
                 for (int e = 0; e < 4; ++e)
                     mine[(g + 8 * (e >> 1)) * DP + out_dim<FP8>(i, e, t)] = R.o[i][e] * back;
             __syncthreads();
-            const bool whole = item_ends && item_first >= begin;
-            const int rows = min(kAttendRows, comp.w.q_len * (int)P.G - b.row0);
-            const bool starts_before = item_first < begin;
+            const int item_first = comp.unit - comp.tile;   // unit of the item's first tile
+            const bool whole = item_ends && item_first >= 0;
+            const int rows = min(kAttendRows, comp.w.q_len * (int)P.G - comp.b.row0);
+            const bool starts_before = item_first < 0;
             float *part = P.parts + (uint64_t)(2u * blockIdx.x + (starts_before ? 0u : 1u)) * C::PART_FLOATS;
             for (int i = tid; i < rows * (DP / 4); i += kAttendThreads) {
                 const int row = i / (DP / 4), d = 4 * (i - row * (DP / 4));
@@ -725,7 +861,7 @@ __global__ void __launch_bounds__(kAttendThreads, DP <= 128 ? 2 : 1) attend_kern
                 for (int w = 0; w < kAttendWarps; ++w) {
                     const float f = fast_exp2(sh_m[w][row] - ref);
                     const float4 x = *reinterpret_cast<const float4 *>(
-                        smem + (w * kAttendStages + stage) * C::STAGE_BYTES + (row * DP + d) * 4);
+                        smem + (w * C::STAGES + stage) * C::STAGE_BYTES + (row * DP + d) * 4);
                     l += f * sh_l[w][row];
                     v.x += f * x.x;
                     v.y += f * x.y;
@@ -734,8 +870,8 @@ __global__ void __launch_bounds__(kAttendThreads, DP <= 128 ? 2 : 1) attend_kern
                 }
                 if (whole) {
                     const float inv = l == 0.f ? 0.f : 1.f / l;
-                    write_row_piece<DP>(P, comp.w, b, row, d, make_float4(v.x * inv, v.y * inv, v.z * inv, v.w * inv));
-                    if (d == 0) write_lse(P, comp.w, b, row, m, l);
+                    write_row_piece<DP>(P, comp.w, comp.b, comp.h, row, d, make_float4(v.x * inv, v.y * inv, v.z * inv, v.w * inv));
+                    if (d == 0) write_lse(P, comp.w, comp.b, comp.h, row, m, l);
                 } else {
                     *reinterpret_cast<float4 *>(part + row * DP + d) = v;
                     if (d == 0) {
@@ -746,9 +882,8 @@ __global__ void __launch_bounds__(kAttendThreads, DP <= 128 ? 2 : 1) attend_kern
             }
             if (!whole) {
                 // the CTAs that share the item: those whose stretches hold its first and its last tile
-                const long long item_last = item_first + comp.w.tiles - 1;
-                const uint32_t c0 = (uint32_t)(((item_first + 1) * ctas - 1) / total);
-                const uint32_t c1 = (uint32_t)(((item_last + 1) * ctas - 1) / total);
+                const uint32_t c0 = (uint32_t)(((begin + item_first + 1) * ctas - 1) / total);
+                const uint32_t c1 = (uint32_t)(((begin + item_first + comp.w.tiles) * ctas - 1) / total);
                 __threadfence();
                 __syncthreads();
                 if (tid == 0) {
@@ -761,38 +896,45 @@ __global__ void __launch_bounds__(kAttendThreads, DP <= 128 ? 2 : 1) attend_kern
                     __threadfence();
                     for (int i = tid; i < rows * (DP / 4); i += kAttendThreads) {
                         const int row = i / (DP / 4), d = 4 * (i - row * (DP / 4));
+                        const float *p0 = P.parts + (uint64_t)(2u * c0 + 1u) * C::PART_FLOATS;   // the first; the others:
+                        auto at = [&](uint32_t c) { return c == c0 ? p0 : P.parts + (uint64_t)(2u * c) * C::PART_FLOATS; };
                         float m = -INFINITY, l = 0.f;
                         float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll 8
+                        for (uint32_t c = c0; c <= c1; ++c) m = fmaxf(m, __ldcg(at(c) + kAttendRows * DP + row));
+                        const float ref = m == -INFINITY ? 0.f : m;
+#pragma unroll 8
                         for (uint32_t c = c0; c <= c1; ++c) {
-                            const float *p = P.parts + (uint64_t)(2u * c + (c == c0 ? 1u : 0u)) * C::PART_FLOATS;
-                            const float pm = __ldcg(p + kAttendRows * DP + row), pl = __ldcg(p + kAttendRows * DP + kAttendRows + row);
+                            const float *p = at(c);
+                            const float f = fast_exp2(__ldcg(p + kAttendRows * DP + row) - ref);
                             const float4 x = __ldcg(reinterpret_cast<const float4 *>(p + row * DP + d));
-                            const float nm = fmaxf(m, pm), ref = nm == -INFINITY ? 0.f : nm;
-                            const float a = fast_exp2(m - ref), f = fast_exp2(pm - ref);
-                            l = a * l + f * pl;
-                            v.x = a * v.x + f * x.x;
-                            v.y = a * v.y + f * x.y;
-                            v.z = a * v.z + f * x.z;
-                            v.w = a * v.w + f * x.w;
-                            m = nm;
+                            l += f * __ldcg(p + kAttendRows * DP + kAttendRows + row);
+                            v.x += f * x.x;
+                            v.y += f * x.y;
+                            v.z += f * x.z;
+                            v.w += f * x.w;
                         }
                         const float inv = l == 0.f ? 0.f : 1.f / l;
-                        write_row_piece<DP>(P, comp.w, b, row, d, make_float4(v.x * inv, v.y * inv, v.z * inv, v.w * inv));
-                        if (d == 0) write_lse(P, comp.w, b, row, m, l);
+                        write_row_piece<DP>(P, comp.w, comp.b, comp.h, row, d, make_float4(v.x * inv, v.y * inv, v.z * inv, v.w * inv));
+                        if (d == 0) write_lse(P, comp.w, comp.b, comp.h, row, m, l);
                     }
                 }
             }
+            if (TMA) fence_async_smem();   // the stage has been written to, and is read
             __syncthreads();
             fresh = true;
         }
         issue(stage);
-        stage = stage + 1 == kAttendStages ? 0 : stage + 1;
-        if (n + 1 < n_tiles) {
-            if (item_ends) item_first += comp.w.tiles;
-            next_tile<C::TILE>(P, comp);
+        if (++stage == C::STAGES) {
+            stage = 0;
+            phase ^= 1u;
         }
+        next_tile<C::TILE>(P, comp);
     }
-    copy_wait<0>();
+    if (!TMA || FP8) copy_wait<0>();
+    if (TMA && sh_abort && lane == 0)   // a wait ran out: what is in flight lands before the CTA ends
+        for (int i = 0; i < C::STAGES && i < loaded; ++i)
+            mbar_drain(full0 + 8u * i, (uint32_t)((loaded - 1 - i) / C::STAGES) & 1u, wait_limit_ns);
 }
 
 }  // namespace gk

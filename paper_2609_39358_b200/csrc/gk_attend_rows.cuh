@@ -22,10 +22,7 @@
 // every block), every CTA takes an equal stretch, parts of a block meet in the workspace.
 #pragma once
 
-#include <cuda.h>  // CUtensorMap
-
 #include "gk_attend.cuh"
-#include "gk_device.cuh"
 
 namespace gk {
 
@@ -48,11 +45,9 @@ struct RowsJoin {
 constexpr uint32_t kRowsHere = 4;
 
 struct RowsParams {
-    CUtensorMap map;      // the layer's K and V: dimension, token, head (token and head as they lie), page, K or V
+    MapDev m;             // copies of up to 128 tokens
     uint32_t tma;         // the map is to be used
-    uint32_t head_first;  // the map's second dimension is the head
-    uint32_t per_tile;    // pages of a tile
-    uint32_t page_rows;   // tokens of a page that one copy takes: min(page_tokens, 128)
+    uint32_t per_tile;    // copies of a tile
     AttendParams a;
     RowsJoin *join;       // one per CTA; null: every block is joined by the CTA that ends last
     float scale_log2;     // |scale| * log2(e); the sign goes into the queries
@@ -83,7 +78,6 @@ __device__ __forceinline__ void tc_fence_before() { asm volatile("tcgen05.fence:
 __device__ __forceinline__ void tc_fence_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
 __device__ __forceinline__ void tc_wait_ld() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
 __device__ __forceinline__ void tc_wait_st() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
-__device__ __forceinline__ void fence_async_smem() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
 
 __device__ __forceinline__ void tc_commit(uint32_t bar)
 {
@@ -369,13 +363,13 @@ __device__ __forceinline__ void rows_fetch(const RowsParams &R, RowsShared &sh, 
     RowsAt a{k, k.t0, 0u, true};
     // the page of this lane in the tile at `a`, or -1
     auto look_up = [&](const RowsAt &a) -> int {
-        const int tok = a.k.sp.first + a.t * kRowsTile + lane * (int)R.page_rows;
-        if (!a.more || lane >= (int)R.per_tile || tok >= a.k.sp.hi || tok + (int)R.page_rows <= a.k.sp.lo || a.k.w.bad) return -1;
+        const int tok = a.k.sp.first + a.t * kRowsTile + lane * (int)R.m.rows;
+        if (!a.more || lane >= (int)R.per_tile || tok >= a.k.sp.hi || tok + (int)R.m.rows <= a.k.sp.lo || a.k.w.bad) return -1;
         return __ldg(P.seqs.page_table + (uint64_t)a.k.s * P.seqs.table_stride + P.cache.by_T.div((uint32_t)tok));
     };
     auto wanted = [&](const RowsAt &a) {
-        const int tok = a.k.sp.first + a.t * kRowsTile + lane * (int)R.page_rows;
-        return lane < (int)R.per_tile && tok < a.k.sp.hi && tok + (int)R.page_rows > a.k.sp.lo;
+        const int tok = a.k.sp.first + a.t * kRowsTile + lane * (int)R.m.rows;
+        return lane < (int)R.per_tile && tok < a.k.sp.hi && tok + (int)R.m.rows > a.k.sp.lo;
     };
     int id = look_up(a);
     uint32_t last_part = 0xffffffffu;
@@ -386,7 +380,7 @@ __device__ __forceinline__ void rows_fetch(const RowsParams &R, RowsShared &sh, 
         }
         const bool have = (uint32_t)id < P.cache.num_pages;
         if (wanted(a) && !have) mark_missing(P, sh, a.part, a.k.s);
-        const uint32_t bytes = (uint32_t)__popc(__ballot_sync(0xffffffffu, have)) * R.page_rows * (FP8 ? DP : DP * 2);
+        const uint32_t bytes = (uint32_t)__popc(__ballot_sync(0xffffffffu, have)) * R.m.rows * (FP8 ? DP : DP * 2);
         const int tok0 = a.k.sp.first + a.t * kRowsTile;
         const int row = R.per_tile == 1u ? tok0 - (int)(P.cache.by_T.div((uint32_t)tok0) * P.cache.T) : 0;
         const int h = a.k.h, page = id;
@@ -411,12 +405,12 @@ __device__ __forceinline__ void rows_fetch(const RowsParams &R, RowsShared &sh, 
             __syncwarp();
             if (have) {
                 const uint32_t dst = smem + (FP8 ? C::RAW_OFF + stage * C::RAW_BYTES : C::KV_OFF + stage * C::TILE_BYTES) +
-                                     (uint32_t)lane * R.page_rows * (FP8 ? DP : 128u);
+                                     (uint32_t)lane * R.m.rows * (FP8 ? DP : 128u);
 #pragma unroll
                 for (int p = 0; p < PIECES; ++p)
                     asm volatile("cp.async.bulk.tensor.5d.shared::cta.global.tile.mbarrier::complete_tx::bytes [%0], "
                                  "[%1, {%2, %3, %4, %5, %6}], [%7];" ::"r"(dst + p * kRowsTile * 128),
-                                 "l"(&R.map), "r"(64 * p), "r"(R.head_first ? h : row), "r"(R.head_first ? row : h), "r"(page), "r"(kv),
+                                 "l"(&R.m.map), "r"(64 * p), "r"(R.m.head_first ? h : row), "r"(R.m.head_first ? row : h), "r"(page), "r"(kv),
                                  "r"(full)
                                  : "memory");
             }
@@ -512,8 +506,8 @@ __device__ __forceinline__ void rows_convert(const RowsParams &R, RowsShared &sh
             for (int i = 0; i < STEPS; ++i) {
                 const uint32_t j = tid + 128u * i, r = j / CPR, c = j % CPR;
                 const uint4 x = *reinterpret_cast<const uint4 *>(src + 16u * j);
-                sts16(dst + tc_piece(r, 2u * c), e4m3_to_f16(x.x), e4m3_to_f16(x.x >> 16), e4m3_to_f16(x.y), e4m3_to_f16(x.y >> 16));
-                sts16(dst + tc_piece(r, 2u * c + 1u), e4m3_to_f16(x.z), e4m3_to_f16(x.z >> 16), e4m3_to_f16(x.w), e4m3_to_f16(x.w >> 16));
+                sts16(dst + tc_piece(r, 2u * c), e4m3_to_f16(x.x), e4m3_to_f16_high(x.x), e4m3_to_f16(x.y), e4m3_to_f16_high(x.y));
+                sts16(dst + tc_piece(r, 2u * c + 1u), e4m3_to_f16(x.z), e4m3_to_f16_high(x.z), e4m3_to_f16(x.w), e4m3_to_f16_high(x.w));
             }
             fence_async_smem();
             mbar_arrive(smem_addr(&sh.full[st]));
@@ -613,8 +607,8 @@ __device__ __forceinline__ void rows_load(const RowsParams &R, RowsShared &sh, R
                         const long long off = row_at[r];
                         uint4 x = make_uint4(0u, 0u, 0u, 0u);
                         if (off >= 0 && c < pieces) x = __ldg(reinterpret_cast<const uint4 *>(base + off + 16u * c));
-                        sts16(dst + tc_piece(r, 2u * c), e4m3_to_f16(x.x), e4m3_to_f16(x.x >> 16), e4m3_to_f16(x.y), e4m3_to_f16(x.y >> 16));
-                        sts16(dst + tc_piece(r, 2u * c + 1u), e4m3_to_f16(x.z), e4m3_to_f16(x.z >> 16), e4m3_to_f16(x.w), e4m3_to_f16(x.w >> 16));
+                        sts16(dst + tc_piece(r, 2u * c), e4m3_to_f16(x.x), e4m3_to_f16_high(x.x), e4m3_to_f16(x.y), e4m3_to_f16_high(x.y));
+                        sts16(dst + tc_piece(r, 2u * c + 1u), e4m3_to_f16(x.z), e4m3_to_f16_high(x.z), e4m3_to_f16(x.w), e4m3_to_f16_high(x.w));
                     }
                     fence_async_smem();
                     mbar_arrive(smem_addr(&sh.full[unit % C::STAGES]));

@@ -127,31 +127,13 @@ int ensure_attention(gk_ctx *c)
     return GK_OK;
 }
 
-template <bool FP8, int DP>
-int launch_attend(gk_ctx *c, const AttendParams &P, cudaStream_t st)
-{
-    using C = AttendCfg<FP8, DP>;
-    static int occ = 0;  // the same on every sm_100 device
-    if (occ == 0) {
-        int n = 0;
-        GK_CUDA(c, cudaFuncSetAttribute(attend_kernel<FP8, DP>, cudaFuncAttributeMaxDynamicSharedMemorySize, C::SMEM));
-        GK_CUDA(c, cudaOccupancyMaxActiveBlocksPerMultiprocessor(&n, attend_kernel<FP8, DP>, kAttendThreads, C::SMEM));
-        occ = n > 0 ? n : 1;
-    }
-    int grid = c->sm_count * occ;
-    if (grid > kAttnMaxCtas) grid = kAttnMaxCtas;
-    attend_kernel<FP8, DP><<<grid, kAttendThreads, C::SMEM, st>>>(P);
-    GK_CUDA(c, cudaGetLastError());
-    c->stats.kernels_launched++;
-    return GK_OK;
-}
-
 typedef CUresult (*EncodeTiled)(CUtensorMap *, CUtensorMapDataType, cuuint32_t, void *, const cuuint64_t *, const cuuint64_t *,
                                 const cuuint32_t *, const cuuint32_t *, CUtensorMapInterleave, CUtensorMapSwizzle,
                                 CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
 
-// The tensor map of a layer's K and V, if its pages tile 128 tokens and its rows are whole copies; P.tma says so.
-void make_map(const gk_ctx *c, const gk_cache *k, RowsParams &P)
+// The tensor map of a layer's K and V with copies of up to `most` tokens; false if pages do not tile that many or rows are
+// not whole copies.
+bool make_map(const gk_ctx *c, const gk_cache *k, const LayerDev &l, uint32_t most, bool swizzle, MapDev &m)
 {
     static const EncodeTiled encode = [] {
         void *f = nullptr;
@@ -163,23 +145,51 @@ void make_map(const gk_ctx *c, const gk_cache *k, RowsParams &P)
         }
         return (EncodeTiled)f;
     }();
-    const LayerDev &l = P.a.cache;
     const bool fp8 = c->geom.dtype == GK_FP8_E4M3;
-    P.tma = 0;
-    if (!encode || (l.D != 64 && l.D != 128)) return;
-    if (l.T % 8 != 0 || (l.T < 128 ? 128 % l.T != 0 : l.T % 128 != 0)) return;
+    if (!encode || (l.D != 64 && l.D != 128)) return false;
+    if (l.T % 8 != 0 || (l.T < most ? most % l.T != 0 : l.T % most != 0)) return false;
     const uint64_t far = 1ull << 39;
-    if (l.page >= far || k->kv_stride >= far || l.page == 0 || k->kv_stride == 0) return;
-    P.head_first = c->gd.head_major ? 0u : 1u;
-    P.page_rows = l.T < 128 ? l.T : 128u;
-    P.per_tile = 128u / P.page_rows;
-    const cuuint64_t dims[5] = {l.D, P.head_first ? l.H : l.T, P.head_first ? l.T : l.H, l.num_pages, 2};
-    const cuuint64_t strides[4] = {P.head_first ? l.head : l.tok, P.head_first ? l.tok : l.head, l.page, k->kv_stride};
-    const cuuint32_t box[5] = {fp8 ? l.D : 64u, P.head_first ? 1u : P.page_rows, P.head_first ? P.page_rows : 1u, 1u, 1u};
+    if (l.page >= far || k->kv_stride >= far || l.page == 0 || k->kv_stride == 0) return false;
+    m.head_first = c->gd.head_major ? 0u : 1u;
+    m.rows = l.T < most ? l.T : most;
+    const cuuint64_t dims[5] = {l.D, m.head_first ? l.H : l.T, m.head_first ? l.T : l.H, l.num_pages, 2};
+    const cuuint64_t strides[4] = {m.head_first ? l.head : l.tok, m.head_first ? l.tok : l.head, l.page, k->kv_stride};
+    const cuuint32_t box[5] = {fp8 ? l.D : 64u, m.head_first ? 1u : m.rows, m.head_first ? m.rows : 1u, 1u, 1u};
     const cuuint32_t ones[5] = {1, 1, 1, 1, 1};
-    P.tma = encode(&P.map, fp8 ? CU_TENSOR_MAP_DATA_TYPE_UINT8 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 5, l.k, dims, strides, box, ones,
-                   CU_TENSOR_MAP_INTERLEAVE_NONE, fp8 ? CU_TENSOR_MAP_SWIZZLE_NONE : CU_TENSOR_MAP_SWIZZLE_128B,
-                   CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+    const CUtensorMapSwizzle sw = !swizzle ? CU_TENSOR_MAP_SWIZZLE_NONE
+                                  : fp8 && l.D == 64 ? CU_TENSOR_MAP_SWIZZLE_64B : CU_TENSOR_MAP_SWIZZLE_128B;
+    return encode(&m.map, fp8 ? CU_TENSOR_MAP_DATA_TYPE_UINT8 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 5, l.k, dims, strides, box, ones,
+                  CU_TENSOR_MAP_INTERLEAVE_NONE, sw, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+template <bool FP8, int DP, bool TMA>
+int launch_attend(gk_ctx *c, const AttendParams &P, const MapDev &m, cudaStream_t st)
+{
+    using C = AttendCfg<FP8, DP, TMA>;
+    static int occ = 0;  // the same on every sm_100 device
+    if (occ == 0) {
+        int n = 0;
+        GK_CUDA(c, cudaFuncSetAttribute(attend_kernel<FP8, DP, TMA>, cudaFuncAttributeMaxDynamicSharedMemorySize, C::SMEM));
+        GK_CUDA(c, cudaOccupancyMaxActiveBlocksPerMultiprocessor(&n, attend_kernel<FP8, DP, TMA>, kAttendThreads, C::SMEM));
+        occ = n > 0 ? n : 1;
+    }
+    int grid = c->sm_count * occ;
+    if (grid > kAttnMaxCtas) grid = kAttnMaxCtas;
+    attend_kernel<FP8, DP, TMA><<<grid, kAttendThreads, C::SMEM, st>>>(P, m, c->d_error, c->wait_limit_ns);
+    GK_CUDA(c, cudaGetLastError());
+    c->stats.kernels_launched++;
+    return GK_OK;
+}
+
+template <bool FP8>
+int attend_few(gk_ctx *c, const gk_cache *cache, const AttendParams &P, cudaStream_t st)
+{
+    const uint32_t D = P.cache.D;
+    MapDev m{};
+    if (D <= 128 && make_map(c, cache, P.cache, AttendCfg<FP8, 64, true>::TK, true, m))
+        return D == 64 ? launch_attend<FP8, 64, true>(c, P, m, st) : launch_attend<FP8, 128, true>(c, P, m, st);
+    return D <= 64 ? launch_attend<FP8, 64, false>(c, P, m, st) : D <= 128 ? launch_attend<FP8, 128, false>(c, P, m, st)
+                                                                          : launch_attend<FP8, 256, false>(c, P, m, st);
 }
 
 template <bool FP8, int DP>
@@ -310,7 +320,8 @@ int gk_attention(gk_ctx *c, const gk_cache *cache, uint32_t layer, const gk_batc
         R.q_sign = scale == 0.f ? 0.f : scale < 0.f ? -1.f : 1.f;
         R.error = c->d_error;
         R.wait_limit_ns = c->wait_limit_ns;
-        make_map(c, cache, R);
+        R.tma = make_map(c, cache, R.a.cache, kRowsTile, c->geom.dtype != GK_FP8_E4M3, R.m);
+        R.per_tile = R.tma ? kRowsTile / R.m.rows : 0;
         // Few blocks mean many CTAs to a block, whose parts one CTA would be long to join; with two blocks per CTA and more
         // that happens in lopsided batches only.
         const uint64_t blocks = ((uint64_t)batch->n_tokens * P.G / kRowsBlock + batch->n_seqs) * c->geom.kv_heads;
@@ -318,11 +329,7 @@ int gk_attention(gk_ctx *c, const gk_cache *cache, uint32_t layer, const gk_batc
         if (c->geom.dtype == GK_FP8_E4M3) return D <= 64 ? launch_rows<true, 64>(c, R, st) : launch_rows<true, 128>(c, R, st);
         return D <= 64 ? launch_rows<false, 64>(c, R, st) : launch_rows<false, 128>(c, R, st);
     }
-    if (c->geom.dtype == GK_FP8_E4M3)
-        return D <= 64 ? launch_attend<true, 64>(c, P, st) : D <= 128 ? launch_attend<true, 128>(c, P, st)
-                                                                    : launch_attend<true, 256>(c, P, st);
-    return D <= 64 ? launch_attend<false, 64>(c, P, st) : D <= 128 ? launch_attend<false, 128>(c, P, st)
-                                                                  : launch_attend<false, 256>(c, P, st);
+    return c->geom.dtype == GK_FP8_E4M3 ? attend_few<true>(c, cache, P, st) : attend_few<false>(c, cache, P, st);
 }
 
 }  // extern "C"
