@@ -193,13 +193,11 @@ def load_library() -> ctypes.CDLL:
     L.gk_ctx_clear_error.argtypes = [vp, vp]
     L.gk_measure_logic_rate.restype = ctypes.c_int
     L.gk_measure_logic_rate.argtypes = [vp, ctypes.POINTER(ctypes.c_double), vp]
-    rows = ctypes.POINTER(CRows)
+    # called for every layer of every step: structures go in as addresses, which ctypes passes on fastest
     L.gk_append.restype = ctypes.c_int
-    L.gk_append.argtypes = [vp, ctypes.POINTER(CCache), u32, ctypes.POINTER(CBatch), ctypes.POINTER(CRope), rows, rows,
-                            u32, rows, rows, vp]
+    L.gk_append.argtypes = [vp, vp, u32, vp, vp, vp, vp, u32, vp, vp, vp]
     L.gk_attention.restype = ctypes.c_int
-    L.gk_attention.argtypes = [vp, ctypes.POINTER(CCache), u32, ctypes.POINTER(CBatch), u32, rows, rows, vp,
-                               ctypes.c_float, u32, u32, vp]
+    L.gk_attention.argtypes = [vp, vp, u32, vp, u32, vp, vp, vp, ctypes.c_float, u32, u32, vp]
     L.gk_debug_status.restype = ctypes.c_int
     L.gk_debug_status.argtypes = [vp, ctypes.POINTER(ctypes.c_uint32)]
     L.gk_debug_range_ok.restype = ctypes.c_int
@@ -241,6 +239,21 @@ class Cache:
                       0 if self.scales is None else self.scales.data_ptr(), self.s_layer_stride,
                       self.s_kv_stride, self.s_page_stride)
 
+    def __setattr__(self, name, value):
+        self.__dict__.pop("_ref", None)
+        self.__dict__[name] = value
+
+    def ref(self):
+        """The address of the C structure, marshalled once for as long as the fields stay what they are (the calls that
+        a step makes for every layer take the same cache)."""
+        d = self.__dict__
+        at = d["data"].data_ptr()
+        known = d.get("_ref")
+        if known is None or known[1] != at:
+            cc = self.c()
+            known = d["_ref"] = (ctypes.addressof(cc), at, cc)
+        return known[0]
+
 
 class Batch:
     """The sequences of a gk_append or gk_attention call (gk_batch in gk.h).
@@ -271,7 +284,7 @@ class Batch:
         self.n_seqs, self.n_tokens, self.max_q_len = n, int(n_tokens), int(max_q_len or n_tokens)
         self._c = CBatch(_ptr(page_table), page_table.stride(0), _ptr(q_start), _ptr(kv_len), _ptr(status), n,
                          self.n_tokens, page_table.shape[1], self.max_q_len)
-        self._ref = ctypes.byref(self._c)
+        self._ref = ctypes.addressof(self._c)
 
 
 class Rope:
@@ -292,7 +305,7 @@ class Rope:
         sec = (ctypes.c_uint32 * 3)(*(list(sections) + [0, 0])[:3])
         self._c = CRope(_ptr(cos_sin), _ptr(positions), cos_sin.shape[0], cos_sin.shape[1], int(interleaved), len(sections),
                         sec, 0)
-        self._ref = ctypes.byref(self._c)
+        self._ref = ctypes.addressof(self._c)
 
 
 def _need(ok: bool, what: str) -> None:
@@ -300,13 +313,23 @@ def _need(ok: bool, what: str) -> None:
         raise GkError(GK_ERR_ARG, "arguments", what)
 
 
-def _rows(x: torch.Tensor, n_tokens: int, heads: int, head_dim: int, name: str):
-    """A CRows reference for a bf16 tensor [n_tokens, heads, head_dim]."""
-    if x.dtype != torch.bfloat16 or x.dim() != 3 or x.shape[0] != n_tokens or x.shape[1] != heads or x.shape[2] != head_dim:
-        _need(False, f"{name}: bf16 [{n_tokens}, {heads}, {head_dim}] is needed, got {x.dtype} {list(x.shape)}")
-    s = x.stride()
-    _need(s[2] == 1, f"{name}: the last dimension must be contiguous")
-    return ctypes.byref(CRows(x.data_ptr(), s[0], s[1]))
+class _Rows:
+    """A CRows structure that is filled anew for every call."""
+
+    def __init__(self):
+        self.c = CRows()
+        self.ref = ctypes.addressof(self.c)
+
+    def of(self, x: torch.Tensor, shape, name: str):
+        """The address for a bf16 tensor of that shape, [n_tokens, heads, head_dim]."""
+        if x.dtype is not torch.bfloat16 or x.shape != shape:
+            _need(False, f"{name}: bf16 {list(shape)} is needed, got {x.dtype} {list(x.shape)}")
+        c = self.c
+        c.data = x.data_ptr()
+        c.token_stride, c.head_stride, last = x.stride()
+        if last != 1:
+            _need(False, f"{name}: the last dimension must be contiguous")
+        return self.ref
 
 
 @dataclass
@@ -325,9 +348,17 @@ def _ptr(t) -> int:
     return t if isinstance(t, int) else t.data_ptr()
 
 
+def _current_stream() -> int:
+    """Handle of torch's current stream (without building a Stream object, where torch can do that)."""
+    raw = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+    if raw is None or not torch.cuda.is_initialized():
+        return torch.cuda.current_stream().cuda_stream
+    return raw(torch.cuda.current_device())
+
+
 def _stream_handle(stream) -> int:
     if stream is None:
-        return torch.cuda.current_stream().cuda_stream
+        return _current_stream()
     if isinstance(stream, int):
         return stream
     return stream.cuda_stream
@@ -376,6 +407,7 @@ class Context:
         if rc != GK_OK:
             raise GkError(rc, "gk_ctx_create")
         self._h = h
+        self._row_args = [_Rows() for _ in range(4)]
         # GK_TUNING="key=value,key=value": tuning keys applied to every new context of the process
         # (gk_ctx_set_tuning; e.g. quad=2 makes every pack and fused restore use page quartets)
         for kv in filter(None, os.environ.get("GK_TUNING", "").split(",")):
@@ -552,17 +584,22 @@ class Context:
                   stream=None):
         """Appends k and v (bf16 [n_tokens, kv_heads, head_dim]) of one layer to the cache, k rotated by ``rope``, and
         writes the rotated q (bf16 [n_tokens, q_heads, head_dim]) to q_out, or over q if that is None."""
-        n, H, D = batch.n_tokens, self.geom.kv_heads, self.geom.head_dim
+        n, geom, rows = batch.n_tokens, self.geom, self._row_args
+        D = geom.head_dim
+        kv = (n, geom.kv_heads, D)
         heads, rq, ro = 0, None, None
         if q is not None:
             heads = q.shape[1] if q.dim() == 3 else 0
-            rq = _rows(q, n, heads, D, "q")
-            ro = rq if q_out is None else _rows(q_out, n, heads, D, "q_out")
-        if rope is not None and rope.positions is not None:
-            _need(rope.positions.numel() == rope.axes * n, "positions: one per axis and token")
-        cc = cache.c()
-        rc = self._lib.gk_append(self._h, ctypes.byref(cc), layer, batch._ref, None if rope is None else rope._ref,
-                                 _rows(k, n, H, D, "k"), _rows(v, n, H, D, "v"), heads, rq, ro, _stream_handle(stream))
+            rq = ro = rows[2].of(q, (n, heads, D), "q")
+            if q_out is not None:
+                ro = rows[3].of(q_out, (n, heads, D), "q_out")
+        at = None
+        if rope is not None:
+            at = rope._ref
+            if rope.positions is not None and rope.positions.numel() != rope.axes * n:
+                _need(False, "positions: one per axis and token")
+        rc = self._lib.gk_append(self._h, cache.ref(), layer, batch._ref, at, rows[0].of(k, kv, "k"), rows[1].of(v, kv, "v"),
+                                 heads, rq, ro, _stream_handle(stream))
         if rc != GK_OK:
             self._check(rc, "gk_append")
 
@@ -571,15 +608,16 @@ class Context:
                      causal: bool = True, stream=None):
         """Attention of q (bf16 [n_tokens, q_heads, head_dim]) over one layer of the cache into out (like q); lse:
         float32 [n_tokens, q_heads].  scale: 1 / sqrt(head_dim) by default.  window: 0 = the whole sequence."""
-        n, D = batch.n_tokens, self.geom.head_dim
+        n, D, rows = batch.n_tokens, self.geom.head_dim, self._row_args
         heads = q.shape[1] if q.dim() == 3 else 0
+        shape = (n, heads, D)
         if lse is not None:
-            _need(lse.dtype == torch.float32 and lse.is_contiguous() and tuple(lse.shape) == (n, heads),
+            _need(lse.dtype == torch.float32 and lse.is_contiguous() and lse.shape == shape[:2],
                   "lse: contiguous float32 [n_tokens, q_heads]")
-        cc = cache.c()
-        rc = self._lib.gk_attention(self._h, ctypes.byref(cc), layer, batch._ref, heads, _rows(q, n, heads, D, "q"),
-                                    _rows(out, n, heads, D, "out"), _ptr(lse), D ** -0.5 if scale is None else scale,
-                                    window, 0 if causal else GK_ATTN_FULL, _stream_handle(stream))
+        rc = self._lib.gk_attention(self._h, cache.ref(), layer, batch._ref, heads, rows[0].of(q, shape, "q"),
+                                    rows[1].of(out, shape, "out"), None if lse is None else lse.data_ptr(),
+                                    D ** -0.5 if scale is None else scale, window, 0 if causal else GK_ATTN_FULL,
+                                    _stream_handle(stream))
         if rc != GK_OK:
             self._check(rc, "gk_attention")
 

@@ -3,6 +3,10 @@
 // The unit of work is an ITEM: 16 dimensions of one head of one token, the 8 + 8 values of 8 rotation
 // pairs (two 16-byte pieces, rotary_dim/2 apart, or adjacent where pairs are), so that a lane loads,
 // turns and stores whole vectors and neighbouring lanes touch neighbouring addresses.
+//
+// The kernel is bound by memory.  A thread keeps its token and its 16 dimensions and walks over the heads, so that the
+// angles, the position and the page are looked up once for all of them, and loads a batch of heads before it
+// works on the first.
 #pragma once
 
 #include "gk_seq.cuh"
@@ -31,32 +35,33 @@ struct AppendParams {
     uint32_t Hq;
     uint32_t chunks;         // items per head row: D / 16
     FastDiv by_chunks;
-    FastDiv by_row;          // items per token of the flat part of the grid
+    uint32_t heads;          // of a token in the token part: queries and, into a bf16 cache, keys and values
+    uint32_t head_lanes;     // threads of a token that share its dimensions: kTokenThreads / chunks
     uint32_t shared_scale;   // fp8: K and V of a page and head share one scale
-    uint32_t unit_ctas, head_groups;  // fp8: CTAs that append pages; the flat part follows them
-    uint32_t unit_slots;
+    uint32_t unit_ctas, unit_every, head_groups;  // fp8: CTAs that append pages, and their distance in the grid
 };
 
-constexpr int kAppendThreads = 128;
-constexpr int kAppendWarps = kAppendThreads / 32;
+constexpr int kAppendThreads = 256;
+constexpr int kTokenThreads = 128;   // of one token: 8 chunks x 16 heads at 128 dimensions
+constexpr int kTokenBatch = 2;       // heads that a thread loads before it works on the first
+constexpr int kUnitHeads = 4;        // fp8: heads of a page that one CTA appends
 
-struct Item {
-    float x[16];
-    uint32_t d0, d1;  // first dimensions of its two pieces
-};
-
-__device__ __forceinline__ void item_dims(const AppendParams &P, uint32_t c, bool rotated, Item &it, bool &turn)
+// First dimensions of the two pieces of chunk c.  Values (which are not rotated) are cut like keys, so that a thread's
+// dimensions are the same in both.
+__device__ __forceinline__ void item_dims(const AppendParams &P, uint32_t c, uint32_t &d0, uint32_t &d1)
 {
-    const uint32_t R = rotated ? P.rope.R : 0u;
-    turn = 16u * c < R;
-    if (turn && !P.rope.interleaved) {
-        it.d0 = 8u * c;
-        it.d1 = (R >> 1) + 8u * c;
+    if (16u * c < P.rope.R && !P.rope.interleaved) {
+        d0 = 8u * c;
+        d1 = (P.rope.R >> 1) + 8u * c;
     } else {
-        it.d0 = 16u * c;
-        it.d1 = 16u * c + 8u;
+        d0 = 16u * c;
+        d1 = 16u * c + 8u;
     }
 }
+
+struct Raw {
+    uint4 a, b;
+};
 
 __device__ __forceinline__ void unpack8(const uint4 &u, float *x)
 {
@@ -79,63 +84,79 @@ __device__ __forceinline__ uint4 pack8(const float *x)
     return make_uint4(w[0], w[1], w[2], w[3]);
 }
 
-// Turns the 8 pairs of chunk c of row i.  Every product is rounded by itself (no fused multiply-add): the
-// result is then the textbook expression's, bit for bit, whatever compiler or library computes that.
-__device__ __forceinline__ void turn_item(const AppendParams &P, uint32_t i, int pos, uint32_t c, Item &it, bool &bad)
+// Cosines and sines of the 8 pairs of a chunk, for one token.
+struct Angles {
+    float cs[8], sn[8];
+    bool bad;  // an index outside the table
+};
+
+__device__ __forceinline__ void load_angles(const AppendParams &P, uint32_t i, int pos, uint32_t c, Angles &a)
 {
     const RopeDev &r = P.rope;
     int row[3] = {pos, pos, pos};
     if (r.positions) {
 #pragma unroll
-        for (int a = 0; a < 3; ++a)
-            if ((uint32_t)a < r.axes) row[a] = __ldg(r.positions + (uint64_t)a * P.seqs.n_tokens + i);
-            else row[a] = row[0];
+        for (int x = 0; x < 3; ++x)
+            if ((uint32_t)x < r.axes) row[x] = __ldg(r.positions + (uint64_t)x * P.seqs.n_tokens + i);
+            else row[x] = row[0];
     }
     const uint32_t p0 = 8u * c, half = r.R >> 1;
-    bad = false;
-#pragma unroll
-    for (int a = 0; a < 3; ++a) bad |= (uint32_t)row[a] >= r.max_pos;
-    float cs[8], sn[8];
-    if (bad) {
-        const float nan = __int_as_float(0x7fc00000);
-#pragma unroll
-        for (int e = 0; e < 16; ++e) it.x[e] = nan;
-        return;
-    }
+    a.bad = (uint32_t)row[0] >= r.max_pos || (uint32_t)row[1] >= r.max_pos || (uint32_t)row[2] >= r.max_pos;
+    if (a.bad) return;
     const uint32_t ax0 = p0 < r.end0 ? 0u : p0 < r.end1 ? 1u : 2u;
     const uint32_t last = p0 + 7u;
     const uint32_t ax7 = last < r.end0 ? 0u : last < r.end1 ? 1u : 2u;
     if (ax0 == ax7) {
         const float *t = r.cos_sin + (uint64_t)(ax0 == 0u ? row[0] : ax0 == 1u ? row[1] : row[2]) * r.R + p0;
-        *reinterpret_cast<float4 *>(cs) = __ldg(reinterpret_cast<const float4 *>(t));
-        *reinterpret_cast<float4 *>(cs + 4) = __ldg(reinterpret_cast<const float4 *>(t) + 1);
-        *reinterpret_cast<float4 *>(sn) = __ldg(reinterpret_cast<const float4 *>(t + half));
-        *reinterpret_cast<float4 *>(sn + 4) = __ldg(reinterpret_cast<const float4 *>(t + half) + 1);
+        const float4 c0 = __ldg(reinterpret_cast<const float4 *>(t)), c1 = __ldg(reinterpret_cast<const float4 *>(t) + 1);
+        const float4 s0 = __ldg(reinterpret_cast<const float4 *>(t + half)), s1 = __ldg(reinterpret_cast<const float4 *>(t + half) + 1);
+        a.cs[0] = c0.x, a.cs[1] = c0.y, a.cs[2] = c0.z, a.cs[3] = c0.w, a.cs[4] = c1.x, a.cs[5] = c1.y, a.cs[6] = c1.z, a.cs[7] = c1.w;
+        a.sn[0] = s0.x, a.sn[1] = s0.y, a.sn[2] = s0.z, a.sn[3] = s0.w, a.sn[4] = s1.x, a.sn[5] = s1.y, a.sn[6] = s1.z, a.sn[7] = s1.w;
     } else {
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
             const uint32_t p = p0 + e;
             const float *t = r.cos_sin + (uint64_t)(p < r.end0 ? row[0] : p < r.end1 ? row[1] : row[2]) * r.R + p;
-            cs[e] = __ldg(t);
-            sn[e] = __ldg(t + half);
+            a.cs[e] = __ldg(t);
+            a.sn[e] = __ldg(t + half);
         }
-    }
-#pragma unroll
-    for (int e = 0; e < 8; ++e) {
-        const int ia = r.interleaved ? 2 * e : e, ib = r.interleaved ? 2 * e + 1 : e + 8;
-        const float a = it.x[ia], b = it.x[ib];
-        it.x[ia] = __fsub_rn(__fmul_rn(a, cs[e]), __fmul_rn(b, sn[e]));
-        it.x[ib] = __fadd_rn(__fmul_rn(b, cs[e]), __fmul_rn(a, sn[e]));
     }
 }
 
-__device__ __forceinline__ void load_item(const RowsDev &r, uint64_t i, uint32_t h, Item &it)
+// Turns the 8 pairs of an item.  Every product is rounded by itself (no fused multiply-add): the result is then the
+// textbook expression's, bit for bit, whatever compiler or library computes that.
+template <bool INTERLEAVED>
+__device__ __forceinline__ void turn_pairs(const Angles &a, float (&x)[16])
+{
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+        const int ia = INTERLEAVED ? 2 * e : e, ib = INTERLEAVED ? 2 * e + 1 : e + 8;
+        const float u = x[ia], v = x[ib];
+        x[ia] = __fsub_rn(__fmul_rn(u, a.cs[e]), __fmul_rn(v, a.sn[e]));
+        x[ib] = __fadd_rn(__fmul_rn(v, a.cs[e]), __fmul_rn(u, a.sn[e]));
+    }
+}
+__device__ __forceinline__ void turn(const AppendParams &P, const Angles &a, float (&x)[16])
+{
+    if (a.bad) {
+#pragma unroll
+        for (int e = 0; e < 16; ++e) x[e] = __int_as_float(0x7fc00000);
+    } else if (P.rope.interleaved) {
+        turn_pairs<true>(a, x);
+    } else {
+        turn_pairs<false>(a, x);
+    }
+}
+
+__device__ __forceinline__ Raw load_item(const RowsDev &r, uint64_t i, uint32_t h, uint32_t d0, uint32_t d1)
 {
     const __nv_bfloat16 *p = r.p + i * r.tok + h * r.head;
-    const uint4 a = __ldg(reinterpret_cast<const uint4 *>(p + it.d0));
-    const uint4 b = __ldg(reinterpret_cast<const uint4 *>(p + it.d1));
-    unpack8(a, it.x);
-    unpack8(b, it.x + 8);
+    return Raw{__ldg(reinterpret_cast<const uint4 *>(p + d0)), __ldg(reinterpret_cast<const uint4 *>(p + d1))};
+}
+__device__ __forceinline__ void unpack(const Raw &r, float (&x)[16])
+{
+    unpack8(r.a, x);
+    unpack8(r.b, x + 8);
 }
 
 // Page id of a token, or -1 (status raised) where the table holds none.
@@ -150,46 +171,65 @@ __device__ __forceinline__ int page_of(const AppendParams &P, uint32_t s, uint32
     return g;
 }
 
-// The flat part: items of queries (and, into a bf16 cache, of keys and values), one per lane.
+// The token part: a token's queries (and, into a bf16 cache, keys and values) by kTokenThreads threads.
 template <bool FP8>
-__device__ __forceinline__ void append_flat(const AppendParams &P, uint32_t idx)
+__device__ __forceinline__ void append_token(const AppendParams &P, uint32_t i, uint32_t tid)
 {
-    const uint32_t i = P.by_row.div(idx);
-    if (i >= P.seqs.n_tokens) return;
-    const uint32_t in_row = idx - i * P.by_row.d;
-    uint32_t h = P.by_chunks.div(in_row);
-    const uint32_t c = in_row - h * P.chunks;
-    int kind = 0;  // query, key, value
-    if (h >= P.Hq) {
-        h -= P.Hq;
-        kind = 1;
-        if (h >= P.cache.H) {
-            h -= P.cache.H;
-            kind = 2;
+    const uint32_t hl = P.by_chunks.div(tid), c = tid - hl * P.chunks;
+    if (i >= P.seqs.n_tokens || hl >= P.head_lanes) return;
+    uint32_t d0, d1;
+    item_dims(P, c, d0, d1);
+    const bool rotated = 16u * c < P.rope.R;
+    Angles ang;
+    ang.bad = false;
+    uint8_t *row = nullptr;   // the token's row of K at head 0
+    bool first = true;
+    for (uint32_t h0 = hl; h0 < P.heads; h0 += kTokenBatch * P.head_lanes) {
+        Raw raw[kTokenBatch];
+#pragma unroll
+        for (int k = 0; k < kTokenBatch; ++k) {
+            const uint32_t h = h0 + k * P.head_lanes;
+            if (h >= P.heads) continue;
+            raw[k] = h < P.Hq ? load_item(P.q, i, h, d0, d1)
+                     : h < P.Hq + P.cache.H ? load_item(P.k, i, h - P.Hq, d0, d1) : load_item(P.v, i, h - P.Hq - P.cache.H, d0, d1);
+        }
+        if (first) {
+            first = false;
+            if (rotated && P.rope.positions) load_angles(P, i, 0, c, ang);   // the sequence does not matter
+            if (!FP8 || ang.bad || (rotated && !P.rope.positions)) {
+                const uint32_t s = seq_of_row(P.seqs, i);
+                const SeqSpan sp = seq_span(P.seqs, s);
+                const int pos = sp.kv - sp.q_len + (int)i - sp.q0;
+                if (rotated && !P.rope.positions) load_angles(P, i, pos, c, ang);
+                if (!FP8 && pos >= 0) {
+                    const uint32_t page = P.cache.by_T.div((uint32_t)pos);
+                    const int g = page_of(P, s, page);
+                    if (g >= 0) row = P.cache.k + (uint64_t)g * P.cache.page + (uint64_t)((uint32_t)pos - page * P.cache.T) * P.cache.tok;
+                }
+                if (ang.bad && P.seqs.status) P.seqs.status[s] = 5;  // GK_SEQ_POSITION
+            }
+        }
+#pragma unroll
+        for (int k = 0; k < kTokenBatch; ++k) {
+            const uint32_t h = h0 + k * P.head_lanes;
+            if (h >= P.heads) continue;
+            const bool value = h >= P.Hq + P.cache.H;
+            uint8_t *dst;
+            if (h < P.Hq) dst = reinterpret_cast<uint8_t *>(P.q_out + (uint64_t)i * P.qo_tok + h * P.qo_head);
+            else if (!row) continue;
+            else if (value) dst = row + (P.cache.v - P.cache.k) + (uint64_t)(h - P.Hq - P.cache.H) * P.cache.head;
+            else dst = row + (uint64_t)(h - P.Hq) * P.cache.head;
+            if (rotated && !value) {
+                float x[16];
+                unpack(raw[k], x);
+                turn(P, ang, x);
+                raw[k].a = pack8(x);
+                raw[k].b = pack8(x + 8);
+            }
+            *reinterpret_cast<uint4 *>(dst + 2u * d0) = raw[k].a;
+            *reinterpret_cast<uint4 *>(dst + 2u * d1) = raw[k].b;
         }
     }
-    Item it;
-    bool turn, bad = false;
-    item_dims(P, c, kind != 2, it, turn);
-    load_item(kind == 0 ? P.q : kind == 1 ? P.k : P.v, i, h, it);
-    const uint32_t s = seq_of_row(P.seqs, i);
-    const SeqSpan sp = seq_span(P.seqs, s);
-    const int pos = sp.kv - sp.q_len + (int)i - sp.q0;
-    if (turn) turn_item(P, i, pos, c, it, bad);
-    if (bad && P.seqs.status) P.seqs.status[s] = 5;  // GK_SEQ_POSITION
-    uint8_t *dst;
-    if (kind == 0) {
-        dst = reinterpret_cast<uint8_t *>(P.q_out + (uint64_t)i * P.qo_tok + h * P.qo_head);
-    } else {
-        if (pos < 0) return;
-        const uint32_t page = P.cache.by_T.div((uint32_t)pos);
-        const int g = page_of(P, s, page);
-        if (g < 0) return;
-        dst = (kind == 1 ? P.cache.k : P.cache.v) + (uint64_t)g * P.cache.page +
-              (uint64_t)((uint32_t)pos - page * P.cache.T) * P.cache.tok + (uint64_t)h * P.cache.head;
-    }
-    *reinterpret_cast<uint4 *>(dst + 2u * it.d0) = pack8(it.x);
-    *reinterpret_cast<uint4 *>(dst + 2u * it.d1) = pack8(it.x + 8);
 }
 
 __device__ __forceinline__ float finite_size(float x)
@@ -198,7 +238,8 @@ __device__ __forceinline__ float finite_size(float x)
     return a <= 3.402823466e38f ? a : 0.f;  // false for infinities and NaN
 }
 
-__device__ __forceinline__ uint2 pack_e4m3(const float *x, float inv)
+// `odd`: there may be infinities, which the conversion would store as the largest value; they become NaN
+__device__ __forceinline__ uint2 pack_e4m3(const float *x, float inv, bool odd)
 {
     uint32_t w[2];
 #pragma unroll
@@ -207,8 +248,8 @@ __device__ __forceinline__ uint2 pack_e4m3(const float *x, float inv)
 #pragma unroll
         for (int j = 0; j < 2; ++j) {
             float2 f = make_float2(__fmul_rn(x[4 * i + 2 * j], inv), __fmul_rn(x[4 * i + 2 * j + 1], inv));
-            if (isinf(f.x)) f.x = __int_as_float(0x7fc00000);  // the conversion would store the largest value
-            if (isinf(f.y)) f.y = __int_as_float(0x7fc00000);
+            if (odd && isinf(f.x)) f.x = __int_as_float(0x7fc00000);
+            if (odd && isinf(f.y)) f.y = __int_as_float(0x7fc00000);
             h[j] = __nv_cvt_float2_to_fp8x2(f, __NV_SATFINITE, __NV_E4M3);
         }
         w[i] = h[0] | (h[1] << 16);
@@ -249,9 +290,19 @@ __device__ __forceinline__ float grown_scale(float big, float old, bool has_rows
     return scale;
 }
 
-// fp8: one warp appends one head (K and V) of one page.  Two passes over the page's new rows (the second finds
-// them in L1/L2): the largest value decides the scale before anything is stored.
-__device__ __forceinline__ void append_unit(const AppendParams &P, uint32_t slot, uint32_t h, int lane)
+struct UnitShared {
+    uint32_t big[2 * kUnitHeads];               // bits of the largest |value|: K of each head, then V
+    uint32_t finite[2 * kUnitHeads];            // of the largest finite one, where that is not the same
+    float inv[2 * kUnitHeads], shrink[2 * kUnitHeads];
+};
+
+// A page that a call appends to, found from its slot.
+struct Unit {
+    uint32_t s, rows, fill, i0;  // sequence, new rows, rows before them, row of the first in the token tensors
+    int g, a;                    // page id, position of the first new row
+};
+
+__device__ __forceinline__ bool find_unit(const AppendParams &P, uint32_t slot, Unit &x)
 {
     const uint32_t T = P.cache.T;
     uint32_t s, u;
@@ -274,91 +325,218 @@ __device__ __forceinline__ void append_unit(const AppendParams &P, uint32_t slot
     const SeqSpan sp = seq_span(P.seqs, s);
     const int start = max(sp.kv - sp.q_len, 0);
     const uint32_t page = P.cache.by_T.div((uint32_t)start) + u;
-    const int a = max(start, (int)(page * T)), b = min(sp.kv, (int)min((uint64_t)(page + 1u) * T, (uint64_t)0x7fffffff));
-    if (a >= b || sp.q_len <= 0) return;
-    const int g = page_of(P, s, page);
-    if (g < 0) return;
-    const uint32_t rows = (uint32_t)(b - a), fill = (uint32_t)a - page * T;
-    const uint32_t i0 = (uint32_t)(sp.q0 + a - (sp.kv - sp.q_len));  // row of the first token
-    const uint32_t n_items = rows * P.chunks;
+    const long long page_at = (long long)page * T;
+    const int a = (int)max((long long)start, page_at), b = (int)min((long long)sp.kv, page_at + T);
+    if (a >= b || sp.q_len <= 0) return false;
+    x.g = page_of(P, s, page);
+    x.s = s;
+    x.a = a;
+    x.rows = (uint32_t)(b - a);
+    x.fill = (uint32_t)(a - page_at);
+    x.i0 = (uint32_t)(sp.q0 + a - (sp.kv - sp.q_len));
+    return x.g >= 0;
+}
 
-    float big[2] = {0.f, 0.f};
-    bool any_bad = false;
-#pragma unroll
-    for (int kv = 0; kv < 2; ++kv) {
+__device__ __forceinline__ void rescale_piece(uint8_t *at, float f)
+{
+    uint4 *w = reinterpret_cast<uint4 *>(at);
+    uint4 x = *w;
+    x.x = rescale_e4m3(x.x, f);
+    x.y = rescale_e4m3(x.y, f);
+    x.z = rescale_e4m3(x.z, f);
+    x.w = rescale_e4m3(x.w, f);
+    *w = x;
+}
+
+// fp8, few new rows a sequence: one warp appends one head (K and V) of one page, in two passes over its new rows.
+__device__ __forceinline__ void append_unit_warp(const AppendParams &P, uint32_t slot, uint32_t h, uint32_t lane)
+{
+    Unit x;
+    if (!find_unit(P, slot, x)) return;
+    const uint32_t n_items = x.rows * P.chunks;
+    float big[2] = {0.f, 0.f}, scale[2] = {1.f, 1.f};
+    for (int pass = 0; pass < 2; ++pass) {
         for (uint32_t j = lane; j < n_items; j += 32u) {
             const uint32_t t = P.by_chunks.div(j), c = j - t * P.chunks;
-            Item it;
-            bool turn, bad = false;
-            item_dims(P, c, kv == 0, it, turn);
-            load_item(kv == 0 ? P.k : P.v, i0 + t, h, it);
-            if (turn) turn_item(P, i0 + t, a + (int)t, c, it, bad);
-            any_bad |= bad;
+            uint32_t d0, d1;
+            item_dims(P, c, d0, d1);
+            const Raw rk = load_item(P.k, x.i0 + t, h, d0, d1), rv = load_item(P.v, x.i0 + t, h, d0, d1);
+            float k[16], v[16];
+            unpack(rk, k);
+            unpack(rv, v);
+            if (16u * c < P.rope.R) {
+                Angles ang;
+                load_angles(P, x.i0 + t, x.a + (int)t, c, ang);
+                if (ang.bad && P.seqs.status) P.seqs.status[x.s] = 5;  // GK_SEQ_POSITION
+                turn(P, ang, k);
+            }
+            if (pass == 0) {
 #pragma unroll
-            for (int e = 0; e < 16; ++e) big[kv] = fmaxf(big[kv], finite_size(it.x[e]));
-        }
-        big[kv] = __uint_as_float(__reduce_max_sync(0xffffffffu, __float_as_uint(big[kv])));
-    }
-    if (any_bad && P.seqs.status) P.seqs.status[s] = 5;  // GK_SEQ_POSITION
-    if (P.shared_scale) big[0] = big[1] = fmaxf(big[0], big[1]);
-
-    float scale[2], shrink[2];
-    scale[0] = grown_scale(big[0], P.cache.ks[(uint64_t)g * P.cache.s_page + h], fill > 0u, shrink[0]);
-    if (P.shared_scale) {
-        scale[1] = scale[0];
-        shrink[1] = shrink[0];
-    } else {
-        scale[1] = grown_scale(big[1], P.cache.vs[(uint64_t)g * P.cache.s_page + h], fill > 0u, shrink[1]);
-    }
-#pragma unroll
-    for (int kv = 0; kv < 2; ++kv) {
-        uint8_t *base = (kv ? P.cache.v : P.cache.k) + (uint64_t)g * P.cache.page + (uint64_t)h * P.cache.head;
-        if (fill > 0u && shrink[kv] != 1.f) {
-            for (uint32_t j = lane; j < fill * P.chunks; j += 32u) {
-                const uint32_t t = P.by_chunks.div(j), c = j - t * P.chunks;
-                uint4 *w = reinterpret_cast<uint4 *>(base + (uint64_t)t * P.cache.tok + 16u * c);
-                uint4 x = *w;
-                x.x = rescale_e4m3(x.x, shrink[kv]);
-                x.y = rescale_e4m3(x.y, shrink[kv]);
-                x.z = rescale_e4m3(x.z, shrink[kv]);
-                x.w = rescale_e4m3(x.w, shrink[kv]);
-                *w = x;
+                for (int e = 0; e < 16; ++e) {
+                    big[0] = fmaxf(big[0], finite_size(k[e]));
+                    big[1] = fmaxf(big[1], finite_size(v[e]));
+                }
+            } else {
+                const uint64_t at = (uint64_t)x.g * P.cache.page + (uint64_t)h * P.cache.head + (uint64_t)(x.fill + t) * P.cache.tok;
+                const float ik = __fdiv_rn(1.f, scale[0]), iv = __fdiv_rn(1.f, scale[1]);
+                *reinterpret_cast<uint2 *>(P.cache.k + at + d0) = pack_e4m3(k, ik, true);
+                *reinterpret_cast<uint2 *>(P.cache.k + at + d1) = pack_e4m3(k + 8, ik, true);
+                *reinterpret_cast<uint2 *>(P.cache.v + at + d0) = pack_e4m3(v, iv, true);
+                *reinterpret_cast<uint2 *>(P.cache.v + at + d1) = pack_e4m3(v + 8, iv, true);
             }
         }
-        const float inv = __fdiv_rn(1.f, scale[kv]);
-        for (uint32_t j = lane; j < n_items; j += 32u) {
-            const uint32_t t = P.by_chunks.div(j), c = j - t * P.chunks;
-            Item it;
-            bool turn, bad;
-            item_dims(P, c, kv == 0, it, turn);
-            load_item(kv == 0 ? P.k : P.v, i0 + t, h, it);
-            if (turn) turn_item(P, i0 + t, a + (int)t, c, it, bad);
-            uint8_t *dst = base + (uint64_t)(fill + t) * P.cache.tok;
-            *reinterpret_cast<uint2 *>(dst + it.d0) = pack_e4m3(it.x, inv);
-            *reinterpret_cast<uint2 *>(dst + it.d1) = pack_e4m3(it.x + 8, inv);
+        if (pass) break;
+#pragma unroll
+        for (int kv = 0; kv < 2; ++kv) big[kv] = __uint_as_float(__reduce_max_sync(0xffffffffu, __float_as_uint(big[kv])));
+        if (P.shared_scale) big[0] = big[1] = fmaxf(big[0], big[1]);
+        float *at[2] = {P.cache.ks + (uint64_t)x.g * P.cache.s_page + h, P.cache.vs + (uint64_t)x.g * P.cache.s_page + h};
+        const float old[2] = {*at[0], *at[1]};
+#pragma unroll
+        for (int kv = 0; kv < 2; ++kv) {
+            float shrink;
+            scale[kv] = grown_scale(big[kv], old[kv], x.fill > 0u, shrink);
+            if (x.fill > 0u && shrink != 1.f) {
+                uint8_t *base = (kv ? P.cache.v : P.cache.k) + (uint64_t)x.g * P.cache.page + (uint64_t)h * P.cache.head;
+                for (uint32_t j = lane; j < x.fill * P.chunks; j += 32u) {
+                    const uint32_t r = P.by_chunks.div(j);
+                    rescale_piece(base + (uint64_t)r * P.cache.tok + 16u * (j - r * P.chunks), shrink);
+                }
+            }
         }
-    }
-    __syncwarp();
-    if (lane == 0) {
-        P.cache.ks[(uint64_t)g * P.cache.s_page + h] = scale[0];
-        if (!P.shared_scale) P.cache.vs[(uint64_t)g * P.cache.s_page + h] = scale[1];
+        __syncwarp();
+        if (lane == 0u) {
+            *at[0] = scale[0];
+            if (!P.shared_scale) *at[1] = scale[1];
+        }
     }
 }
 
-template <bool FP8>
-__global__ void __launch_bounds__(kAppendThreads) append_kernel(const AppendParams P)
+// fp8: a CTA appends kUnitHeads heads (K and V) of one page.  The largest value decides the scale before anything is
+// stored, so there are two passes over the new rows; the second finds them in L1 or L2.  (Keeping them in registers in
+// between unrolls the passes over the heads into more code than the instruction cache holds.)
+__device__ __forceinline__ void append_unit(const AppendParams &P, UnitShared &sh, uint32_t slot, uint32_t h0, uint32_t tid)
+{
+    Unit un;
+    if (!find_unit(P, slot, un)) return;
+    const uint32_t n_items = un.rows * P.chunks, heads = min((uint32_t)kUnitHeads, P.cache.H - h0);
+    float *scale_at = nullptr;   // thread k < 8: the scale of K or V of one head
+    float old = 1.f;
+    if (tid < 2u * kUnitHeads) {
+        sh.big[tid] = sh.finite[tid] = 0u;
+        if (tid % kUnitHeads < heads) {
+            scale_at = (tid < kUnitHeads ? P.cache.ks : P.cache.vs) + (uint64_t)un.g * P.cache.s_page + h0 + tid % kUnitHeads;
+            if (un.fill) old = *scale_at;
+        }
+    }
+    __syncthreads();
+
+    // every new row's item of every head to body(k, x): k < kUnitHeads keys, from there on values
+    uint32_t d0 = 0, d1 = 0, t = 0;
+    bool active = false;
+    auto each = [&](auto body) {
+#pragma unroll 1
+        for (uint32_t j0 = 0; j0 < n_items; j0 += kAppendThreads) {
+            const uint32_t j = j0 + tid;
+            active = j < n_items;
+            t = P.by_chunks.div(active ? j : 0u);
+            const uint32_t c = (active ? j : 0u) - t * P.chunks;
+            item_dims(P, c, d0, d1);
+            Raw next = load_item(P.k, un.i0 + t, h0, d0, d1);
+            Angles ang;
+            ang.bad = false;
+            const bool rotated = 16u * c < P.rope.R;
+            if (rotated) load_angles(P, un.i0 + t, un.a + (int)t, c, ang);
+            if (ang.bad && P.seqs.status) P.seqs.status[un.s] = 5;  // GK_SEQ_POSITION
+#pragma unroll 1
+            for (uint32_t n = 0; n < 2u * heads; ++n) {
+                const Raw raw = next;
+                const bool value = n >= heads;
+                const uint32_t m = n + 1u;
+                if (m < 2u * heads)
+                    next = load_item(m >= heads ? P.v : P.k, un.i0 + t, h0 + (m >= heads ? m - heads : m), d0, d1);
+                float x[16];
+                unpack(raw, x);
+                if (rotated && !value) turn(P, ang, x);
+                body(value ? kUnitHeads + n - heads : n, x);
+            }
+        }
+    };
+    // the largest |value|: NaN does not count, an infinity shows and has the finite values looked through again
+    each([&](uint32_t k, float (&x)[16]) {
+        float m = 0.f;
+#pragma unroll
+        for (int e = 0; e < 16; ++e) m = fmaxf(m, fabsf(x[e]));
+        const uint32_t w = __reduce_max_sync(0xffffffffu, active ? __float_as_uint(m) : 0u);
+        if ((tid & 31u) == 0u && w) atomicMax(&sh.big[k], w);
+    });
+    __syncthreads();
+    bool odd = false;
+#pragma unroll
+    for (int k = 0; k < 2 * kUnitHeads; ++k) odd |= sh.big[k] >= 0x7f800000u;
+    if (odd) {
+        each([&](uint32_t k, float (&x)[16]) {
+            float m = 0.f;
+#pragma unroll
+            for (int e = 0; e < 16; ++e) m = fmaxf(m, finite_size(x[e]));
+            if (active) atomicMax(&sh.finite[k], __float_as_uint(m));
+        });
+        __syncthreads();
+    }
+    if (scale_at) {
+        const uint32_t *top = odd ? sh.finite : sh.big;
+        uint32_t m = top[tid];
+        if (P.shared_scale) m = max(m, top[tid ^ kUnitHeads]);
+        float shrink;
+        const float scale = grown_scale(__uint_as_float(m), old, un.fill > 0u, shrink);
+        sh.inv[tid] = __fdiv_rn(1.f, scale);
+        sh.shrink[tid] = shrink;
+        if (!(P.shared_scale && tid >= kUnitHeads)) *scale_at = scale;
+    }
+    __syncthreads();
+    const uint64_t page = (uint64_t)un.g * P.cache.page;
+    if (un.fill > 0u) {
+        // earlier rows of heads whose scale has grown
+        for (uint32_t k = 0; k < 2u * kUnitHeads; ++k) {
+            if (k % kUnitHeads >= heads || sh.shrink[k] == 1.f) continue;
+            uint8_t *base = (k < kUnitHeads ? P.cache.k : P.cache.v) + page + (uint64_t)(h0 + k % kUnitHeads) * P.cache.head;
+            for (uint32_t j = tid; j < un.fill * P.chunks; j += kAppendThreads) {
+                const uint32_t r = P.by_chunks.div(j);
+                rescale_piece(base + (uint64_t)r * P.cache.tok + 16u * (j - r * P.chunks), sh.shrink[k]);
+            }
+        }
+    }
+    each([&](uint32_t k, float (&x)[16]) {
+        uint8_t *dst = (k < kUnitHeads ? P.cache.k : P.cache.v) + page + (uint64_t)(h0 + k % kUnitHeads) * P.cache.head +
+                       (uint64_t)(un.fill + t) * P.cache.tok;
+        const uint2 a = pack_e4m3(x, sh.inv[k], odd), b = pack_e4m3(x + 8, sh.inv[k], odd);
+        if (!active) return;
+        *reinterpret_cast<uint2 *>(dst + d0) = a;
+        *reinterpret_cast<uint2 *>(dst + d1) = b;
+    });
+}
+
+// FEW (fp8): a warp appends a page and head; else a CTA a page and four heads.  CTAs that append pages are spread among those of
+// the token part, one every `unit_every`: pages wait on their scales, and the queries' traffic fills the memory meanwhile.
+template <bool FP8, bool FEW>
+__global__ void __launch_bounds__(kAppendThreads, 4) append_kernel(const __grid_constant__ AppendParams P)
 {
     uint32_t cta = blockIdx.x;
     if (FP8) {
-        if (cta < P.unit_ctas) {
-            const uint32_t slot = cta / P.head_groups;
-            const uint32_t h = (cta - slot * P.head_groups) * kAppendWarps + (threadIdx.x >> 5);
-            if (h < P.cache.H) append_unit(P, slot, h, threadIdx.x & 31);
+        __shared__ UnitShared sh;
+        const uint32_t n = cta / P.unit_every;
+        if (n < P.unit_ctas && n * P.unit_every == cta) {
+            const uint32_t slot = n / P.head_groups, group = n - slot * P.head_groups;
+            if (!FEW) {
+                append_unit(P, sh, slot, group * kUnitHeads, threadIdx.x);
+            } else {
+                const uint32_t h = group * (kAppendThreads / 32) + threadIdx.x / 32u;
+                if (h < P.cache.H) append_unit_warp(P, slot, h, threadIdx.x & 31u);
+            }
             return;
         }
-        cta -= P.unit_ctas;
+        cta -= min(n + 1u, P.unit_ctas);
     }
-    append_flat<FP8>(P, cta * kAppendThreads + threadIdx.x);
+    append_token<FP8>(P, cta * (kAppendThreads / kTokenThreads) + threadIdx.x / kTokenThreads, threadIdx.x % kTokenThreads);
 }
 
 }  // namespace gk

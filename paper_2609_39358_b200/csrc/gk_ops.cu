@@ -254,24 +254,34 @@ int gk_append(gk_ctx *c, const gk_cache *dst, uint32_t layer, const gk_batch *ba
     const bool fp8 = c->geom.dtype == GK_FP8_E4M3;
     P.chunks = c->geom.head_dim / 16;
     P.by_chunks = FastDiv::make(P.chunks);
-    const uint64_t per_token = ((uint64_t)P.Hq + (fp8 ? 0u : 2u * c->geom.kv_heads)) * P.chunks;
-    const uint64_t items = per_token * batch->n_tokens;
-    if (per_token > 0x7fffffffull || items > 0x7fffff00ull) return fail(c, GK_ERR_TOO_LARGE, "append: too many tokens times heads");
-    P.by_row = FastDiv::make(per_token ? (uint32_t)per_token : 1u);
-    uint64_t grid = (items + kAppendThreads - 1) / kAppendThreads;
-    if (fp8) {
-        P.shared_scale = c->geom.scale_kv == 1;
-        P.head_groups = (c->geom.kv_heads + kAppendWarps - 1) / kAppendWarps;
-        // a sequence of n rows touches at most n / T + 2 pages
-        const uint64_t slots = batch->q_start ? batch->n_tokens / c->geom.page_tokens + 2ull * batch->n_seqs : batch->n_seqs;
-        if (slots * P.head_groups + grid > 0x7fffffffull) return fail(c, GK_ERR_TOO_LARGE, "append: too many pages times heads");
-        P.unit_slots = (uint32_t)slots;
-        P.unit_ctas = (uint32_t)(slots * P.head_groups);
-        grid += P.unit_ctas;
-        append_kernel<true><<<(unsigned)grid, kAppendThreads, 0, (cudaStream_t)stream>>>(P);
-    } else {
-        append_kernel<false><<<(unsigned)grid, kAppendThreads, 0, (cudaStream_t)stream>>>(P);
+    const uint64_t heads = (uint64_t)P.Hq + (fp8 ? 0u : 2u * c->geom.kv_heads);
+    if (heads > 0x7fffffffull) return fail(c, GK_ERR_TOO_LARGE, "append: too many heads");
+    P.heads = (uint32_t)heads;
+    P.head_lanes = kTokenThreads / P.chunks;
+    constexpr uint32_t kTokens = kAppendThreads / kTokenThreads;
+    const uint64_t token_ctas = heads ? ((uint64_t)batch->n_tokens + kTokens - 1) / kTokens : 0;
+    const cudaStream_t st = (cudaStream_t)stream;
+    if (!fp8) {
+        append_kernel<false, false><<<(unsigned)token_ctas, kAppendThreads, 0, st>>>(P);
+        GK_CUDA(c, cudaGetLastError());
+        c->stats.kernels_launched++;
+        return GK_OK;
     }
+    P.shared_scale = c->geom.scale_kv == 1;
+    // a sequence of n rows touches at most n / T + 2 pages
+    const uint64_t slots = batch->q_start ? batch->n_tokens / c->geom.page_tokens + 2ull * batch->n_seqs : batch->n_seqs;
+    const uint32_t max_q = batch->q_start ? (batch->max_q_len ? batch->max_q_len : batch->n_tokens) : 1u;
+    // Few rows a sequence leave most of a CTA idle: a warp per page and head then, a CTA per page and four heads for more.
+    const bool by_warp = (uint64_t)max_q * P.chunks <= 32u;
+    const uint32_t per_cta = by_warp ? kAppendThreads / 32 : kUnitHeads;
+    P.head_groups = (c->geom.kv_heads + per_cta - 1) / per_cta;
+    if (slots * P.head_groups + token_ctas > 0x7fffffffull) return fail(c, GK_ERR_TOO_LARGE, "append: too many pages times heads");
+    const uint32_t page_ctas = (uint32_t)(slots * P.head_groups);
+    P.unit_ctas = page_ctas;
+    const uint32_t all = page_ctas + (uint32_t)token_ctas;
+    P.unit_every = all / page_ctas;
+    if (by_warp) append_kernel<true, true><<<all, kAppendThreads, 0, st>>>(P);
+    else append_kernel<true, false><<<all, kAppendThreads, 0, st>>>(P);
     GK_CUDA(c, cudaGetLastError());
     c->stats.kernels_launched++;
     return GK_OK;
