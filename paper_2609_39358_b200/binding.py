@@ -313,6 +313,10 @@ def _need(ok: bool, what: str) -> None:
         raise GkError(GK_ERR_ARG, "arguments", what)
 
 
+# handle of torch's current stream on a device, without building a Stream object where torch can do that
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda device: torch.cuda.current_stream(device).cuda_stream)
+
+
 class _Rows:
     """A CRows structure that is filled anew for every call."""
 
@@ -348,17 +352,9 @@ def _ptr(t) -> int:
     return t if isinstance(t, int) else t.data_ptr()
 
 
-def _current_stream() -> int:
-    """Handle of torch's current stream (without building a Stream object, where torch can do that)."""
-    raw = getattr(torch._C, "_cuda_getCurrentRawStream", None)
-    if raw is None or not torch.cuda.is_initialized():
-        return torch.cuda.current_stream().cuda_stream
-    return raw(torch.cuda.current_device())
-
-
 def _stream_handle(stream) -> int:
     if stream is None:
-        return _current_stream()
+        return torch.cuda.current_stream().cuda_stream
     if isinstance(stream, int):
         return stream
     return stream.cuda_stream
@@ -599,7 +595,7 @@ class Context:
             if rope.positions is not None and rope.positions.numel() != rope.axes * n:
                 _need(False, "positions: one per axis and token")
         rc = self._lib.gk_append(self._h, cache.ref(), layer, batch._ref, at, rows[0].of(k, kv, "k"), rows[1].of(v, kv, "v"),
-                                 heads, rq, ro, _stream_handle(stream))
+                                 heads, rq, ro, _raw_stream(self.device) if stream is None else _stream_handle(stream))
         if rc != GK_OK:
             self._check(rc, "gk_append")
 
@@ -617,7 +613,7 @@ class Context:
         rc = self._lib.gk_attention(self._h, cache.ref(), layer, batch._ref, heads, rows[0].of(q, shape, "q"),
                                     rows[1].of(out, shape, "out"), None if lse is None else lse.data_ptr(),
                                     D ** -0.5 if scale is None else scale, window, 0 if causal else GK_ATTN_FULL,
-                                    _stream_handle(stream))
+                                    _raw_stream(self.device) if stream is None else _stream_handle(stream))
         if rc != GK_OK:
             self._check(rc, "gk_attention")
 

@@ -521,6 +521,7 @@ template <bool FP8, bool FEW>
 __global__ void __launch_bounds__(kAppendThreads, 4) append_kernel(const __grid_constant__ AppendParams P)
 {
     uint32_t cta = blockIdx.x;
+    grid_begin();
     if (FP8) {
         __shared__ UnitShared sh;
         const uint32_t n = cta / P.unit_every;

@@ -685,6 +685,7 @@ __global__ void __launch_bounds__(kAttendThreads, AttendCfg<FP8, DP, TMA>::CTAS)
     __shared__ float sh_m[kAttendWarps][kAttendRows], sh_l[kAttendWarps][kAttendRows];
     __shared__ uint32_t sh_last;
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+    grid_begin();
     if (TMA && tid == 0) {
         for (int i = 0; i < kAttendWarps * C::STAGES; ++i) mbar_init(smem_addr(&sh_full[0][0] + i), 1);
         sh_abort = 0u;

@@ -1261,7 +1261,7 @@ template <int DP>
 __global__ void __launch_bounds__(128) join_rows_kernel(const __grid_constant__ RowsParams R)
 {
     const AttendParams &P = R.a;
-    asm volatile("griddepcontrol.wait;" ::: "memory");
+    grid_begin();
     const RowsJoin j = R.join[blockIdx.x];
     const int d = 32 * (threadIdx.x >> 5), prow = (int)blockIdx.y * 32 + (threadIdx.x & 31);
     if (j.parts == 0 || d >= (int)P.cache.D) return;
@@ -1287,9 +1287,8 @@ __global__ void __launch_bounds__(kRowsThreads, 1) attend_rows_kernel(const __gr
     const int tid = threadIdx.x, warp = __shfl_sync(0xffffffffu, tid >> 5, 0), lane = tid & 31;
     uint8_t *smem_ptr = smem_raw + ((1024u - (smem_addr(smem_raw) & 1023u)) & 1023u);
     const uint32_t smem = smem_addr(smem_ptr);
+    grid_begin();
     if (R.join && tid == 0) R.join[blockIdx.x].parts = 0u;   // tid 0 also enters a block there
-    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
-
     // the length of the line
     long long total = 0;
     for (uint32_t s0 = 0; s0 < P.seqs.n_seqs; s0 += kRowsThreads) {

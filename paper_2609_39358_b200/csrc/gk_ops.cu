@@ -98,6 +98,27 @@ int check_rope(gk_ctx *c, const gk_rope *r, RopeDev *out)
     return GK_OK;
 }
 
+// `early` launches with programmatic stream serialisation: the grid may be set up while the one before it on the stream drains.  Every
+// kernel here begins with grid_begin() (gk_seq.cuh), which waits for that one's end, so the stream's order stands.
+template <class... Params, class... Args>
+int launch(gk_ctx *c, bool early, void (*kernel)(Params...), dim3 grid, unsigned threads, size_t smem, cudaStream_t st,
+           const Args &...args)
+{
+    cudaLaunchConfig_t cfg{};
+    cfg.gridDim = grid;
+    cfg.blockDim = dim3(threads);
+    cfg.dynamicSmemBytes = smem;
+    cfg.stream = st;
+    cudaLaunchAttribute at{};
+    at.id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    at.val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = &at;
+    cfg.numAttrs = early ? 1 : 0;
+    GK_CUDA(c, cudaLaunchKernelEx(&cfg, kernel, args...));
+    c->stats.kernels_launched++;
+    return GK_OK;
+}
+
 // Workspace of gk_attention: join counters, blocks for the join kernel, two partial results per CTA of the largest grid.
 constexpr size_t kAttnCounterBytes = 4096;
 constexpr size_t kAttnJoinBytes = 16384;
@@ -175,10 +196,7 @@ int launch_attend(gk_ctx *c, const AttendParams &P, const MapDev &m, cudaStream_
     }
     int grid = c->sm_count * occ;
     if (grid > kAttnMaxCtas) grid = kAttnMaxCtas;
-    attend_kernel<FP8, DP, TMA><<<grid, kAttendThreads, C::SMEM, st>>>(P, m, c->d_error, c->wait_limit_ns);
-    GK_CUDA(c, cudaGetLastError());
-    c->stats.kernels_launched++;
-    return GK_OK;
+    return launch(c, true, attend_kernel<FP8, DP, TMA>, dim3(grid), kAttendThreads, C::SMEM, st, P, m, c->d_error, c->wait_limit_ns);
 }
 
 template <bool FP8>
@@ -205,23 +223,9 @@ int launch_rows(gk_ctx *c, const RowsParams &P, cudaStream_t st)
         GK_CUDA(c, cudaFuncSetAttribute(attend_rows_kernel<FP8, DP>, cudaFuncAttributeMaxDynamicSharedMemorySize, C::SMEM));
         ready = true;
     }
-    attend_rows_kernel<FP8, DP><<<c->sm_count, kRowsThreads, C::SMEM, st>>>(P);
-    GK_CUDA(c, cudaGetLastError());
-    c->stats.kernels_launched++;
-    if (P.join) {
-        cudaLaunchConfig_t cfg{};
-        cfg.gridDim = dim3(c->sm_count, kRowsBlock / 32);
-        cfg.blockDim = dim3(DP);
-        cfg.stream = st;
-        cudaLaunchAttribute at{};
-        at.id = cudaLaunchAttributeProgrammaticStreamSerialization;
-        at.val.programmaticStreamSerializationAllowed = 1;
-        cfg.attrs = &at;
-        cfg.numAttrs = 1;
-        GK_CUDA(c, cudaLaunchKernelEx(&cfg, join_rows_kernel<DP>, P));
-        c->stats.kernels_launched++;
-    }
-    return GK_OK;
+    int rc = launch(c, false, attend_rows_kernel<FP8, DP>, dim3(c->sm_count), kRowsThreads, C::SMEM, st, P);
+    if (rc == GK_OK && P.join) rc = launch(c, true, join_rows_kernel<DP>, dim3(c->sm_count, kRowsBlock / 32), DP, 0, st, P);
+    return rc;
 }
 
 }  // namespace
@@ -261,12 +265,7 @@ int gk_append(gk_ctx *c, const gk_cache *dst, uint32_t layer, const gk_batch *ba
     constexpr uint32_t kTokens = kAppendThreads / kTokenThreads;
     const uint64_t token_ctas = heads ? ((uint64_t)batch->n_tokens + kTokens - 1) / kTokens : 0;
     const cudaStream_t st = (cudaStream_t)stream;
-    if (!fp8) {
-        append_kernel<false, false><<<(unsigned)token_ctas, kAppendThreads, 0, st>>>(P);
-        GK_CUDA(c, cudaGetLastError());
-        c->stats.kernels_launched++;
-        return GK_OK;
-    }
+    if (!fp8) return launch(c, true, append_kernel<false, false>, dim3((unsigned)token_ctas), kAppendThreads, 0, st, P);
     P.shared_scale = c->geom.scale_kv == 1;
     // a sequence of n rows touches at most n / T + 2 pages
     const uint64_t slots = batch->q_start ? batch->n_tokens / c->geom.page_tokens + 2ull * batch->n_seqs : batch->n_seqs;
@@ -280,11 +279,7 @@ int gk_append(gk_ctx *c, const gk_cache *dst, uint32_t layer, const gk_batch *ba
     P.unit_ctas = page_ctas;
     const uint32_t all = page_ctas + (uint32_t)token_ctas;
     P.unit_every = all / page_ctas;
-    if (by_warp) append_kernel<true, true><<<all, kAppendThreads, 0, st>>>(P);
-    else append_kernel<true, false><<<all, kAppendThreads, 0, st>>>(P);
-    GK_CUDA(c, cudaGetLastError());
-    c->stats.kernels_launched++;
-    return GK_OK;
+    return launch(c, true, by_warp ? append_kernel<true, true> : append_kernel<true, false>, dim3(all), kAppendThreads, 0, st, P);
 }
 
 int gk_attention(gk_ctx *c, const gk_cache *cache, uint32_t layer, const gk_batch *batch, uint32_t q_heads,

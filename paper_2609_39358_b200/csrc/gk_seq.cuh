@@ -52,6 +52,14 @@ struct SeqSpan {
     int q0, q_len, kv;
 };
 
+// First in every kernel: the grid before this one on the stream has ended and its writes are there; the next one may be
+// set up (it waits here in its turn).
+__device__ __forceinline__ void grid_begin()
+{
+    asm volatile("griddepcontrol.wait;" ::: "memory");
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+}
+
 // Rows and tokens of sequence s.  Row offsets are clamped to the token tensors, so that a bad offset
 // array can never lead outside them.
 __device__ __forceinline__ SeqSpan seq_span(const SeqsDev &b, uint32_t s)
