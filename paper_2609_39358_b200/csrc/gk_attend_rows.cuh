@@ -502,16 +502,23 @@ __device__ __forceinline__ void rows_convert(const RowsParams &R, RowsShared &sh
             if (!ok) continue;
             const uint8_t *src = smem_ptr + C::RAW_OFF + rs * C::RAW_BYTES;
             const uint32_t dst = smem + C::KV_OFF + st * C::TILE_BYTES;
-#pragma unroll 4
+            uint4 x[STEPS];
+#pragma unroll
+            for (int i = 0; i < STEPS; ++i) x[i] = *reinterpret_cast<const uint4 *>(src + 16u * (tid + 128u * i));
+            mbar_arrive(smem_addr(&sh.raw_empty[rs]));
+#pragma unroll
             for (int i = 0; i < STEPS; ++i) {
                 const uint32_t j = tid + 128u * i, r = j / CPR, c = j % CPR;
-                const uint4 x = *reinterpret_cast<const uint4 *>(src + 16u * j);
-                sts16(dst + tc_piece(r, 2u * c), e4m3_to_f16(x.x), e4m3_to_f16_high(x.x), e4m3_to_f16(x.y), e4m3_to_f16_high(x.y));
-                sts16(dst + tc_piece(r, 2u * c + 1u), e4m3_to_f16(x.z), e4m3_to_f16_high(x.z), e4m3_to_f16(x.w), e4m3_to_f16_high(x.w));
+                // lanes of the upper half of the dimensions, whose pieces lie in the same banks, store theirs the other way round
+                const bool swap = (c >> 2) & 1u;
+                const uint32_t lo[4] = {e4m3_to_f16(x[i].x), e4m3_to_f16_high(x[i].x), e4m3_to_f16(x[i].y), e4m3_to_f16_high(x[i].y)};
+                const uint32_t hi[4] = {e4m3_to_f16(x[i].z), e4m3_to_f16_high(x[i].z), e4m3_to_f16(x[i].w), e4m3_to_f16_high(x[i].w)};
+                const uint32_t first = dst + tc_piece(r, 2u * c + (swap ? 1u : 0u)), second = dst + tc_piece(r, 2u * c + (swap ? 0u : 1u));
+                sts16(first, swap ? hi[0] : lo[0], swap ? hi[1] : lo[1], swap ? hi[2] : lo[2], swap ? hi[3] : lo[3]);
+                sts16(second, swap ? lo[0] : hi[0], swap ? lo[1] : hi[1], swap ? lo[2] : hi[2], swap ? lo[3] : hi[3]);
             }
             fence_async_smem();
             mbar_arrive(smem_addr(&sh.full[st]));
-            mbar_arrive(smem_addr(&sh.raw_empty[rs]));
         }
     }
 }
