@@ -6,7 +6,13 @@
 // in one pass with a running maximum m: when it rises, what has been summed is multiplied by
 // exp(m_old - m_new).
 //
-// Work.  An ITEM is (sequence, 16 query rows, key head); a query row is a (token, head of the group) pair, so
+// Products.  mma.sync multiplies tiles of 16 x 16 with tiles of 16 x 8; the 16 rows are tokens (scores) and
+// dimensions (outputs) and the 8 columns are query rows, so that a group of up to 8 heads leaves nothing idle:
+//   S^T = K Q^T    (tokens x rows)        O^T += V^T P^T    (dimensions x rows)
+// tcgen05.mma has at least 64 rows on either side of K; a step has 8 query rows, and its products take a fifth of the
+// time that its bytes do.
+//
+// Work.  An ITEM is (sequence, 8 query rows, key head); a query row is a (token, head of the group) pair, so
 // the heads that share a key head share its loads.  An item's tokens are cut into tiles of 4 warps x TK
 // tokens; the tiles of all items lie in one line, and every CTA takes an equal stretch of that
 // line.  No length, ragged or not, leaves a part of the GPU idle.  A CTA's stretch may begin and end inside an
@@ -50,19 +56,14 @@ struct AttendParams {
 
 constexpr int kAttendWarps = 4;
 constexpr int kAttendThreads = 32 * kAttendWarps;
-constexpr int kAttendRows = 16;
-
-#ifndef GK_ATTEND_STAGES
-#define GK_ATTEND_STAGES 3
-#endif
-#ifndef GK_ATTEND_CTAS
-#define GK_ATTEND_CTAS 2
-#endif
+constexpr int kAttendRows = 8;
 
 template <bool FP8, int DP, bool TMA>
 struct AttendCfg {
-    static constexpr int STAGES = TMA ? GK_ATTEND_STAGES : 3;
-    static constexpr int CTAS = TMA ? GK_ATTEND_CTAS : DP <= 128 ? 2 : 1;   // per SM
+    // Copies in flight against warps to compute: bf16 is bound by its bytes and does best with 2 CTAs of 3 stages (97,561
+    // tokens 78 us; 90 us with 3 CTAs of 2), fp8 by its instructions, with 3 CTAs of 2 (32 x 2,100 tokens 64 us; 78 us).
+    static constexpr int STAGES = FP8 ? 2 : 3;
+    static constexpr int CTAS = DP > 128 ? 1 : FP8 ? 3 : 2;   // per SM
     static constexpr int E = FP8 ? 1 : 2;
     static constexpr int TK = FP8 ? 32 : 16;         // tokens of a stage
     static constexpr int TILE = kAttendWarps * TK;   // tokens of a tile
@@ -138,6 +139,14 @@ __device__ __forceinline__ uint32_t f16x2(float lo, float hi)
     const __half2 b = __floats2half2_rn(lo, hi);
     return *reinterpret_cast<const uint32_t *>(&b);
 }
+// transposes an 8 x 8 tile of 16-bit values: row g, columns 2t and 2t + 1 of a lane become column g, rows 2t and 2t + 1
+__device__ __forceinline__ uint32_t movmatrix_trans(uint32_t a)
+{
+    uint32_t d;
+    asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(d) : "r"(a));
+    return d;
+}
+
 // two e4m3 values as f16, exactly: the low half of w, and the high half
 __device__ __forceinline__ uint32_t e4m3_to_f16(uint32_t w)
 {
@@ -169,7 +178,7 @@ struct SeqWork {
     int q0, q_len, kv;  // rows, tokens
     int first;          // first token of the first tile
     int tiles;          // tiles of every item of the sequence
-    int blocks;         // of 16 rows
+    int blocks;         // of 8 rows
     bool bad;           // longer than its page table
 };
 
@@ -198,7 +207,7 @@ __device__ __forceinline__ long long seq_units(const AttendParams &P, const SeqW
     return (long long)w.blocks * P.cache.H * (w.tiles + kAttendCost);
 }
 
-// Rows of a 16-row block and the tokens that they attend to.
+// Rows of a block and the tokens that they attend to.
 struct BlockSpan {
     int row0;    // first row (token * G + head of the group)
     int lo, hi;  // tokens that some row of the block attends to
@@ -323,93 +332,91 @@ __device__ __forceinline__ bool load_stage(const AttendParams &P, const MapDev &
     return __any_sync(0xffffffffu, m.want && !have);
 }
 
-// Rows g and g + 8 of a 16-row block, as a lane sees them.
+// Lane 4g + t holds query row g while queries are loaded, and rows 2t and 2t + 1 of scores, weights and outputs.
 struct LaneRows {
-    int lo[2], hi[2];  // tokens that the row attends to (none: hi <= lo)
+    int lo[2], hi[2];  // tokens that the rows 2t, 2t + 1 attend to (none: hi <= lo)
     float mul[2];      // scale * log2(e), times the row's power of two with f16 queries
 };
 
 template <bool FP8, int DP>
 __device__ __forceinline__ void load_queries(const AttendParams &P, const SeqWork &w, const BlockSpan &b, int h, int lane,
-                                             uint32_t (&qa)[DP / 16][4], LaneRows &lr)
+                                             uint32_t (&qb)[DP / 16][2], LaneRows &lr)
 {
     const int g = lane >> 2, t = lane & 3;
     const int rows = w.q_len * (int)P.G, at = w.kv - w.q_len;
     const uint32_t D = P.cache.D;
+    const bool live = b.row0 + g < rows;
+    const uint32_t r = live ? (uint32_t)(b.row0 + g) : 0u, j = P.by_G.div(r);
+    const __nv_bfloat16 *p = P.q + (uint64_t)(w.q0 + (int)j) * P.q_tok + (uint64_t)((uint32_t)h * P.G + (r - j * P.G)) * P.q_head;
+    float up = 1.f;
+    if (!FP8) {
+        // k-step s, dimensions 16s + 2t, +1 and 16s + 8 + 2t, +1
 #pragma unroll
-    for (int half = 0; half < 2; ++half) {
-        const int r = b.row0 + g + 8 * half;
-        const bool live = r < rows;
-        const uint32_t j = P.by_G.div((uint32_t)(live ? r : 0));
-        const uint32_t head = (uint32_t)h * P.G + (uint32_t)((live ? r : 0) - (int)(j * P.G));
-        const __nv_bfloat16 *p = P.q + (uint64_t)(w.q0 + j) * P.q_tok + (uint64_t)head * P.q_head;
-        const int pos = at + (int)j;
-        lr.hi[half] = !live ? 0 : P.causal ? max(0, pos + 1) : w.kv;
-        lr.lo[half] = P.window ? (int)max(0ll, (long long)pos + 1 - (long long)P.window) : 0;
-        lr.mul[half] = P.scale_log2;
-        if (!FP8) {
-            // k-step s, dimensions 16s + 2t, +1 and 16s + 8 + 2t, +1
+        for (int s = 0; s < DP / 16; ++s)
 #pragma unroll
-            for (int s = 0; s < DP / 16; ++s)
-#pragma unroll
-                for (int e = 0; e < 2; ++e) {
-                    const uint32_t d = 16u * s + 8u * e + 2u * t;
-                    qa[s][half + 2 * e] = live && d < D ? __ldg(reinterpret_cast<const uint32_t *>(p + d)) : 0u;
-                }
-        } else {
-            // A lane's 16-byte pieces of a key row are 16 consecutive dimensions, so queries are dealt out
-            // alike (the order of the dimensions in a dot product is free): k-step 4j + s takes dimensions
-            // 64j + 16t + 4s ..+3.  bf16 queries become f16 after a division by the row's power of two: exact
-            // but for values 2^-14 below the row's largest.
-            uint32_t raw[DP / 16][2];
-            uint32_t top = 0;
-#pragma unroll
-            for (int s = 0; s < DP / 16; ++s) {
-                const uint32_t d = 64u * (s / 4) + 16u * t + 4u * (s % 4);
-                uint2 u = make_uint2(0u, 0u);
-                if (live && d < D) u = __ldg(reinterpret_cast<const uint2 *>(p + d));
-                raw[s][0] = u.x;
-                raw[s][1] = u.y;
-#pragma unroll
-                for (int e = 0; e < 2; ++e) {
-                    const uint32_t a = raw[s][e] & 0x7fffu, c = (raw[s][e] >> 16) & 0x7fffu;
-                    if (a < 0x7f80u) top = max(top, a);
-                    if (c < 0x7f80u) top = max(top, c);
-                }
+            for (int e = 0; e < 2; ++e) {
+                const uint32_t d = 16u * s + 8u * e + 2u * t;
+                qb[s][e] = live && d < D ? __ldg(reinterpret_cast<const uint32_t *>(p + d)) : 0u;
             }
-            top = max(top, __shfl_xor_sync(0xffffffffu, top, 1));
-            top = max(top, __shfl_xor_sync(0xffffffffu, top, 2));
-            const int ex = min(max((int)(top >> 7) - 127, -126), 126);
-            const float down = __uint_as_float((uint32_t)(127 - ex) << 23);
-            lr.mul[half] *= __uint_as_float((uint32_t)(127 + ex) << 23);
+    } else {
+        // A lane's 16-byte pieces of a key row are 16 consecutive dimensions, so queries are dealt out alike (the order of the
+        // dimensions in a dot product is free): k-step 4j + s takes dimensions 64j + 16t + 4s ..+3.  bf16 queries become f16
+        // after a division by the row's power of two: exact but for values 2^-14 below the row's largest.
+        uint32_t top = 0;
 #pragma unroll
-            for (int s = 0; s < DP / 16; ++s)
-#pragma unroll
-                for (int e = 0; e < 2; ++e)
-                    qa[s][half + 2 * e] = f16x2(__uint_as_float(raw[s][e] << 16) * down,
-                                                __uint_as_float(raw[s][e] & 0xffff0000u) * down);
+        for (int s = 0; s < DP / 16; ++s) {
+            const uint32_t d = 64u * (s / 4) + 16u * t + 4u * (s % 4);
+            uint2 u = make_uint2(0u, 0u);
+            if (live && d < D) u = __ldg(reinterpret_cast<const uint2 *>(p + d));
+            qb[s][0] = u.x;
+            qb[s][1] = u.y;
         }
+#pragma unroll
+        for (int s = 0; s < DP / 16; ++s)
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+                const uint32_t a = qb[s][e] & 0x7fffu, c = (qb[s][e] >> 16) & 0x7fffu;
+                if (a < 0x7f80u) top = max(top, a);
+                if (c < 0x7f80u) top = max(top, c);
+            }
+        top = max(top, __shfl_xor_sync(0xffffffffu, top, 1));
+        top = max(top, __shfl_xor_sync(0xffffffffu, top, 2));
+        const int ex = min(max((int)(top >> 7) - 127, -126), 126);
+        const float down = __uint_as_float((uint32_t)(127 - ex) << 23);
+        up = __uint_as_float((uint32_t)(127 + ex) << 23);
+#pragma unroll
+        for (int s = 0; s < DP / 16; ++s)
+#pragma unroll
+            for (int e = 0; e < 2; ++e)
+                qb[s][e] = f16x2(__uint_as_float(qb[s][e] << 16) * down, __uint_as_float(qb[s][e] & 0xffff0000u) * down);
+    }
+#pragma unroll
+    for (int e = 0; e < 2; ++e) {
+        const int row = b.row0 + 2 * t + e;
+        const int pos = at + (int)P.by_G.div((uint32_t)(row < rows ? row : 0));
+        lr.hi[e] = row >= rows ? 0 : P.causal ? max(0, pos + 1) : w.kv;
+        lr.lo[e] = P.window ? (int)max(0ll, (long long)pos + 1 - (long long)P.window) : 0;
+        lr.mul[e] = P.scale_log2 * __shfl_sync(0xffffffffu, up, 4 * (2 * t + e));
     }
 }
 
 // A warp's running state of one item.
 template <int DP>
 struct Running {
-    float o[DP / 8][4];
-    float m[2], l[2];  // rows g, g + 8; l is this lane's share of the sum
-    float vref;        // fp8: outputs are held divided by this, the largest value scale seen
+    float o[DP / 16][4];   // 16 dimensions of rows 2t, 2t + 1; see out_dim
+    float m[2], l[2];      // rows 2t, 2t + 1; l is this lane's share of the sum
+    float vref;            // fp8: outputs are held divided by this, the largest value scale seen
 };
 
 // f16 weights are multiplied by 2^12 so that small ones keep their bits; outputs carry the factor until the end.
 constexpr float kWeightUp = 4096.f;
 
-// Dimension of element e of accumulator n, for lane position t.
+// Dimension of element e (row 2t + (e & 1)) of accumulator n, for lane 4g + t.
 template <bool FP8>
-__device__ __forceinline__ int out_dim(int n, int e, int t)
+__device__ __forceinline__ int out_dim(int n, int e, int g)
 {
-    // fp8: accumulators 2i and 2i + 1 hold the even and the odd dimensions of 16i ..+15
-    if (FP8) return 16 * (n >> 1) + 2 * (2 * t + (e & 1)) + (n & 1);
-    return 8 * n + 2 * t + (e & 1);
+    // fp8: rows g and g + 8 of a tile are its even and its odd dimensions
+    return FP8 ? 16 * n + 2 * g + (e >> 1) : 16 * n + g + 8 * (e >> 1);
 }
 
 // Does a stage's V hold an infinity or NaN?
@@ -427,99 +434,106 @@ __device__ __forceinline__ bool values_not_finite(const uint8_t *v, int lane)
 }
 
 template <bool FP8, int DP, bool TMA>
-__device__ __forceinline__ void add_values_by_element(const uint8_t *v, const float (&s)[AttendCfg<FP8, DP, TMA>::TK / 8][4],
+__device__ __forceinline__ void add_values_by_element(const uint8_t *v, const float (&s)[AttendCfg<FP8, DP, TMA>::TK / 16][4],
                                                       Running<DP> &R, int lane)
 {
     using C = AttendCfg<FP8, DP, TMA>;
-    const int t = lane & 3;
+    const int g = lane >> 2, t = lane & 3;
 #pragma unroll
-    for (int n8 = 0; n8 < C::TK / 8; ++n8)
+    for (int m = 0; m < C::TK / 16; ++m)
 #pragma unroll 1
-        for (int k = 0; k < 8; ++k) {
+        for (int k = 0; k < 16; ++k) {   // token 16m + k is with lane 4 (k & 7) + t
             float w[2];
 #pragma unroll
-            for (int half = 0; half < 2; ++half)
-                w[half] = __shfl_sync(0xffffffffu, (k & 1) ? s[n8][1 + 2 * half] : s[n8][2 * half], (lane & ~3) | (k >> 1));
+            for (int e = 0; e < 2; ++e) w[e] = __shfl_sync(0xffffffffu, k < 8 ? s[m][e] : s[m][2 + e], 4 * (k & 7) + t);
 #pragma unroll
-            for (int n = 0; n < DP / 8; ++n)
+            for (int n = 0; n < DP / 16; ++n)
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
-                    const int d = out_dim<FP8>(n, e, t) * C::E;
-                    const uint8_t *p = v + piece<FP8, DP, TMA>(8 * n8 + k, d / 16) + d % 16;
+                    const int d = out_dim<FP8>(n, e, g) * C::E;
+                    const uint8_t *p = v + piece<FP8, DP, TMA>(16 * m + k, d / 16) + d % 16;
                     float x;
                     if (FP8) x = __half2float(__half(__nv_cvt_fp8_to_halfraw(*p, __NV_E4M3)));
                     else x = __bfloat162float(*reinterpret_cast<const __nv_bfloat16 *>(p));
-                    if (w[e >> 1] != 0.f) R.o[n][e] += w[e >> 1] * x;
+                    if (w[e & 1] != 0.f) R.o[n][e] += w[e & 1] * x;
                 }
         }
 }
 
+// One stage: TK tokens from tok0 on.  `partial`: not every row attends to all of them; blo, bhi: some row of the block does.
 template <bool FP8, int DP, bool TMA>
 __device__ __forceinline__ void attend_stage(const AttendParams &P, uint32_t stage, const uint8_t *stage_ptr, const float *scales, int tok0,
-                                             const uint32_t (&qa)[DP / 16][4], const LaneRows &lr, Running<DP> &R, bool partial, int blo, int bhi, int lane)
+                                             const uint32_t (&qb)[DP / 16][2], const LaneRows &lr, Running<DP> &R, bool partial, int blo,
+                                             int bhi, int lane)
 {
     using C = AttendCfg<FP8, DP, TMA>;
-    const int t = lane & 3;
-    float s[C::TK / 8][4];
+    constexpr int MT = C::TK / 16;   // tiles of 16 tokens
+    const int g = lane >> 2;
+    float s[MT][4];   // token g (elements 0, 1) and g + 8 (2, 3) of a tile, rows 2t and 2t + 1
 #pragma unroll
-    for (int n = 0; n < C::TK / 8; ++n)
+    for (int m = 0; m < MT; ++m)
 #pragma unroll
-        for (int e = 0; e < 4; ++e) s[n][e] = 0.f;
-    // scores: operands of all tokens first, then the tiles of 8 tokens in turn, so that no product waits for the last one
+        for (int e = 0; e < 4; ++e) s[m][e] = 0.f;
+    // scores; two sums per tile, so that a product does not wait for the one before it
+    float s2[MT][4];
+#pragma unroll
+    for (int m = 0; m < MT; ++m)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) s2[m][e] = 0.f;
     if (!FP8) {
 #pragma unroll
-        for (int k = 0; k < DP / 32; k += 2) {
-            uint32_t b[2][C::TK / 8][4];
+        for (int k = 0; k < DP / 16; k += 2) {
+            uint32_t a[2][MT][4];
 #pragma unroll
             for (int j = 0; j < 2; ++j)
 #pragma unroll
-                for (int n = 0; n < C::TK / 8; ++n)
-                    ldmatrix4(b[j][n], stage + piece<FP8, DP, TMA>(8u * n + (lane & 7), 4u * (k + j) + (lane >> 3)));
+                for (int m = 0; m < MT; ++m)
+                    ldmatrix4(a[j][m], stage + piece<FP8, DP, TMA>(16u * m + (lane & 15), 2u * (k + j) + (lane >> 4)));
 #pragma unroll
-            for (int j = 0; j < 4; ++j)
-#pragma unroll
-                for (int n = 0; n < C::TK / 8; ++n)
-                    mma16816<false>(s[n], qa[2 * k + j], b[j >> 1][n][2 * (j & 1)], b[j >> 1][n][2 * (j & 1) + 1]);
+            for (int m = 0; m < MT; ++m) {
+                mma16816<false>(s[m], a[0][m], qb[k][0], qb[k][1]);
+                mma16816<false>(s2[m], a[1][m], qb[k + 1][0], qb[k + 1][1]);
+            }
         }
     } else {
 #pragma unroll
         for (int j = 0; j < DP / 64; ++j) {
-            uint4 u[C::TK / 8];
+            uint4 u[MT][2];
 #pragma unroll
-            for (int n = 0; n < C::TK / 8; ++n)
-                u[n] = *reinterpret_cast<const uint4 *>(stage_ptr + piece<FP8, DP, TMA>(8u * n + (lane >> 2), 4u * j + t));
+            for (int m = 0; m < MT; ++m)
+#pragma unroll
+                for (int e = 0; e < 2; ++e)
+                    u[m][e] = *reinterpret_cast<const uint4 *>(stage_ptr + piece<FP8, DP, TMA>(16u * m + 8u * e + g, 4u * j + (lane & 3)));
 #pragma unroll
             for (int k = 0; k < 4; ++k)
 #pragma unroll
-                for (int n = 0; n < C::TK / 8; ++n) {
-                    const uint32_t w = k == 0 ? u[n].x : k == 1 ? u[n].y : k == 2 ? u[n].z : u[n].w;
-                    mma16816<true>(s[n], qa[4 * j + k], e4m3_to_f16(w), e4m3_to_f16_high(w));
+                for (int m = 0; m < MT; ++m) {
+                    const uint32_t w0 = k == 0 ? u[m][0].x : k == 1 ? u[m][0].y : k == 2 ? u[m][0].z : u[m][0].w;
+                    const uint32_t w1 = k == 0 ? u[m][1].x : k == 1 ? u[m][1].y : k == 2 ? u[m][1].z : u[m][1].w;
+                    const uint32_t a[4] = {e4m3_to_f16(w0), e4m3_to_f16(w1), e4m3_to_f16_high(w0), e4m3_to_f16_high(w1)};
+                    mma16816<true>(k & 1 ? s2[m] : s[m], a, qb[4 * j + k][0], qb[4 * j + k][1]);
                 }
         }
     }
     // scale, mask, running maximum
     float top[2] = {-INFINITY, -INFINITY};
 #pragma unroll
-    for (int n = 0; n < C::TK / 8; ++n) {
+    for (int m = 0; m < MT; ++m) {
+        float ks[2] = {1.f, 1.f};
         if (FP8) {
-            const float2 f = *reinterpret_cast<const float2 *>(scales + 8 * n + 2 * t);
-            s[n][0] *= f.x * lr.mul[0];
-            s[n][1] *= f.y * lr.mul[0];
-            s[n][2] *= f.x * lr.mul[1];
-            s[n][3] *= f.y * lr.mul[1];
-        } else {
-#pragma unroll
-            for (int e = 0; e < 4; ++e) s[n][e] *= lr.mul[e >> 1];
+            ks[0] = scales[16 * m + g];
+            ks[1] = scales[16 * m + 8 + g];
         }
-        if (partial) {
 #pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                const int tok = tok0 + 8 * n + 2 * t + (e & 1);
-                if (tok < lr.lo[e >> 1] || tok >= lr.hi[e >> 1]) s[n][e] = -INFINITY;
+        for (int e = 0; e < 4; ++e) {
+            s[m][e] += s2[m][e];
+            s[m][e] *= FP8 ? ks[e >> 1] * lr.mul[e & 1] : lr.mul[e & 1];
+            if (partial) {
+                const int tok = tok0 + 16 * m + 8 * (e >> 1) + g;
+                if (tok < lr.lo[e & 1] || tok >= lr.hi[e & 1]) s[m][e] = -INFINITY;
             }
+            top[e & 1] = fmaxf(top[e & 1], s[m][e]);
         }
-#pragma unroll
-        for (int half = 0; half < 2; ++half) top[half] = fmaxf(top[half], fmaxf(s[n][2 * half], s[n][2 * half + 1]));
     }
     float vtop = 0.f;
     bool odd = false;   // a value scale that is no number: it may reach only what attends to its tokens
@@ -533,29 +547,26 @@ __device__ __forceinline__ void attend_stage(const AttendParams &P, uint32_t sta
             vtop = __uint_as_float(__reduce_max_sync(0xffffffffu, __float_as_uint(vtop)));
         }
     }
-    bool rise = FP8 && vtop > R.vref;
-#pragma unroll
-    for (int half = 0; half < 2; ++half) {
-        top[half] = fmaxf(top[half], __shfl_xor_sync(0xffffffffu, top[half], 1));
-        top[half] = fmaxf(top[half], __shfl_xor_sync(0xffffffffu, top[half], 2));
-        rise |= top[half] > R.m[half];
-    }
-    if (__any_sync(0xffffffffu, rise)) {
+    // A maximum that one lane sees is the row's business only if it rises: mostly nobody has one, and the rows' maxima need
+    // not be gathered.
+    if (__any_sync(0xffffffffu, top[0] > R.m[0] || top[1] > R.m[1] || (FP8 && vtop > R.vref))) {
         float down_v = 1.f;
         if (FP8 && vtop > R.vref) {
             down_v = R.vref / vtop;
             R.vref = vtop;
         }
 #pragma unroll
-        for (int half = 0; half < 2; ++half) {
-            const float m = fmaxf(R.m[half], top[half]);
-            const float down = m == R.m[half] ? 1.f : fast_exp2(R.m[half] - m);
-            R.m[half] = m;
-            R.l[half] *= down;
+        for (int e = 0; e < 2; ++e) {
 #pragma unroll
-            for (int n = 0; n < DP / 8; ++n) {
-                R.o[n][2 * half] *= down * down_v;
-                R.o[n][2 * half + 1] *= down * down_v;
+            for (int o = 4; o < 32; o <<= 1) top[e] = fmaxf(top[e], __shfl_xor_sync(0xffffffffu, top[e], o));
+            const float m = fmaxf(R.m[e], top[e]);
+            const float down = m == R.m[e] ? 1.f : fast_exp2(R.m[e] - m);
+            R.m[e] = m;
+            R.l[e] *= down;
+#pragma unroll
+            for (int n = 0; n < DP / 16; ++n) {
+                R.o[n][e] *= down * down_v;
+                R.o[n][2 + e] *= down * down_v;
             }
         }
     }
@@ -563,27 +574,17 @@ __device__ __forceinline__ void attend_stage(const AttendParams &P, uint32_t sta
     const float ref[2] = {R.m[0] == -INFINITY ? 0.f : R.m[0], R.m[1] == -INFINITY ? 0.f : R.m[1]};
     const float up = FP8 ? (R.vref > 0.f ? kWeightUp / R.vref : 0.f) : 1.f;
 #pragma unroll
-    for (int n = 0; n < C::TK / 8; ++n)
+    for (int m = 0; m < MT; ++m) {
+        float vs[2] = {1.f, 1.f};
+        if (FP8) {
+            vs[0] = scales[C::TK + 16 * m + g] * up;
+            vs[1] = scales[C::TK + 16 * m + 8 + g] * up;
+        }
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
-            s[n][e] = fast_exp2(s[n][e] - ref[e >> 1]);
-            R.l[e >> 1] += s[n][e];
-        }
-    if (FP8) {
-#pragma unroll
-        for (int n = 0; n < C::TK / 8; ++n) {
-            const float2 f = *reinterpret_cast<const float2 *>(scales + C::TK + 8 * n + 2 * t);
-            const float v0 = f.x * up, v1 = f.y * up;
-            const float z[4] = {s[n][0], s[n][1], s[n][2], s[n][3]};
-            s[n][0] *= v0;
-            s[n][1] *= v1;
-            s[n][2] *= v0;
-            s[n][3] *= v1;
-            if (odd) {
-#pragma unroll
-                for (int e = 0; e < 4; ++e)
-                    if (z[e] == 0.f) s[n][e] = 0.f;
-            }
+            const float w = fast_exp2(s[m][e] - ref[e & 1]);
+            R.l[e & 1] += w;
+            s[m][e] = !FP8 ? w : odd && w == 0.f ? 0.f : w * vs[e >> 1];
         }
     }
     // outputs
@@ -605,45 +606,44 @@ __device__ __forceinline__ void attend_stage(const AttendParams &P, uint32_t sta
         return;
     }
 #pragma unroll
-    for (int k = 0; k < C::TK / 16; ++k) {
-        const uint32_t r = 16u * k + (lane & 15);
+    for (int m = 0; m < MT; ++m) {
         if (!FP8) {
             // a weight goes in as its upper 16 bits and the bf16 of the rest: rounding weights to 8 bits would add as much
             // error as the rounding of the result, and the tensor pipe has the time.  Neither part is negative, nor 0
             // unless the weight is, so that an infinite V stays what it is.
-            uint32_t hi[4], lo[4];
+            uint32_t hi[2], lo[2];
 #pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                const float a = s[2 * k + (e >> 1)][2 * (e & 1)], b = s[2 * k + (e >> 1)][2 * (e & 1) + 1];
-                hi[e] = __byte_perm(__float_as_uint(a), __float_as_uint(b), 0x7632);
+            for (int e = 0; e < 2; ++e) {
+                const float a = s[m][2 * e], b = s[m][2 * e + 1];
+                hi[e] = movmatrix_trans(__byte_perm(__float_as_uint(a), __float_as_uint(b), 0x7632));
                 const float la = a - __uint_as_float(__float_as_uint(a) & 0xffff0000u);
                 const float lb = b - __uint_as_float(__float_as_uint(b) & 0xffff0000u);
-                lo[e] = bf16x2(fmaxf(la, a * 0x1p-24f), fmaxf(lb, b * 0x1p-24f));
+                lo[e] = movmatrix_trans(bf16x2(fmaxf(la, a * 0x1p-24f), fmaxf(lb, b * 0x1p-24f)));
             }
 #pragma unroll
-            for (int n = 0; n < DP / 16; ++n) {
-                uint32_t b[4];
-                ldmatrix4_trans(b, vbase + piece<FP8, DP, TMA>(r, 2u * n + (lane >> 4)));
-                mma16816<false>(R.o[2 * n], hi, b[0], b[1]);
-                mma16816<false>(R.o[2 * n + 1], hi, b[2], b[3]);
-                mma16816<false>(R.o[2 * n], lo, b[0], b[1]);
-                mma16816<false>(R.o[2 * n + 1], lo, b[2], b[3]);
+            for (int n = 0; n < DP / 16; n += 2) {
+                uint32_t v[2][4];
+#pragma unroll
+                for (int j = 0; j < 2; ++j)
+                    ldmatrix4_trans(v[j], vbase + piece<FP8, DP, TMA>(16u * m + (lane & 7) + 8u * (lane >> 4), 2u * (n + j) + ((lane >> 3) & 1)));
+                mma16816<false>(R.o[n], v[0], hi[0], hi[1]);
+                mma16816<false>(R.o[n + 1], v[1], hi[0], hi[1]);
+                mma16816<false>(R.o[n], v[0], lo[0], lo[1]);
+                mma16816<false>(R.o[n + 1], v[1], lo[0], lo[1]);
             }
         } else {
-            uint32_t a[4];
+            const uint32_t b0 = movmatrix_trans(f16x2(s[m][0], s[m][1])), b1 = movmatrix_trans(f16x2(s[m][2], s[m][3]));
+            // transposing 16-bit pairs of e4m3 values: a register holds dimensions 2g, 2g + 1 of token 2t, then of token
+            // 2t + 1; its bytes 0, 2 and 1, 3 are the even dimension's two tokens and the odd one's
 #pragma unroll
-            for (int e = 0; e < 4; ++e) a[e] = f16x2(s[2 * k + (e >> 1)][2 * (e & 1)], s[2 * k + (e >> 1)][2 * (e & 1) + 1]);
-            // transposing 16-bit pairs of e4m3 values: a register holds dimensions 2g, 2g + 1 of token 2t, then of
-            // token 2t + 1; its bytes 0, 2 and 1, 3 are the operands for the even and the odd dimensions
+            for (int n = 0; n < DP / 16; n += 2) {
+                uint32_t v[4];
+                ldmatrix4_trans(v, vbase + piece<FP8, DP, TMA>(16u * m + (lane & 15), (uint32_t)n + (lane >> 4)));
 #pragma unroll
-            for (int n = 0; n < DP / 32; ++n) {
-                uint32_t b[4];
-                ldmatrix4_trans(b, vbase + piece<FP8, DP, TMA>(r, 2u * n + (lane >> 4)));
-#pragma unroll
-                for (int e = 0; e < 2; ++e) {
-                    const uint32_t x = __byte_perm(b[2 * e], 0, 0x3120), y = __byte_perm(b[2 * e + 1], 0, 0x3120);
-                    mma16816<true>(R.o[4 * n + 2 * e], a, e4m3_to_f16(x), e4m3_to_f16(y));
-                    mma16816<true>(R.o[4 * n + 2 * e + 1], a, e4m3_to_f16_high(x), e4m3_to_f16_high(y));
+                for (int j = 0; j < 2; ++j) {
+                    const uint32_t x = __byte_perm(v[2 * j], 0, 0x3120), y = __byte_perm(v[2 * j + 1], 0, 0x3120);
+                    const uint32_t a[4] = {e4m3_to_f16(x), e4m3_to_f16_high(x), e4m3_to_f16(y), e4m3_to_f16_high(y)};
+                    mma16816<true>(R.o[n + j], a, b0, b1);
                 }
             }
         }
@@ -797,7 +797,7 @@ __global__ void __launch_bounds__(kAttendThreads, AttendCfg<FP8, DP, TMA>::CTAS)
 #pragma unroll
     for (int i = 0; i < C::STAGES; ++i) issue(i);
 
-    uint32_t qa[DP / 16][4];
+    uint32_t qb[DP / 16][2];
     LaneRows lr;
     Running<DP> R;
     bool fresh = true;
@@ -806,9 +806,9 @@ __global__ void __launch_bounds__(kAttendThreads, AttendCfg<FP8, DP, TMA>::CTAS)
     const int g = lane >> 2, t = lane & 3;
     while (comp.unit < units) {
         if (fresh) {
-            load_queries<FP8, DP>(P, comp.w, comp.b, comp.h, lane, qa, lr);
+            load_queries<FP8, DP>(P, comp.w, comp.b, comp.h, lane, qb, lr);
 #pragma unroll
-            for (int i = 0; i < DP / 8; ++i)
+            for (int i = 0; i < DP / 16; ++i)
 #pragma unroll
                 for (int e = 0; e < 4; ++e) R.o[i][e] = 0.f;
             R.m[0] = R.m[1] = -INFINITY;
@@ -821,7 +821,7 @@ __global__ void __launch_bounds__(kAttendThreads, AttendCfg<FP8, DP, TMA>::CTAS)
         __syncwarp();
         const int tok0 = comp.w.first + comp.tile * C::TILE + warp * C::TK;
         attend_stage<FP8, DP, TMA>(P, ring + stage * C::STAGE_BYTES, ring_ptr + stage * C::STAGE_BYTES,
-                                   reinterpret_cast<const float *>(scale_ptr + stage * C::SCALE_BYTES), tok0, qa, lr, R,
+                                   reinterpret_cast<const float *>(scale_ptr + stage * C::SCALE_BYTES), tok0, qb, lr, R,
                                    tok0 < comp.b.all_lo || tok0 + C::TK > comp.b.all_hi, comp.b.lo, comp.b.hi, lane);
         if ((bad_stages >> stage) & 1u) R.l[0] = R.l[1] = __int_as_float(0x7fc00000);
         __syncwarp();
@@ -830,20 +830,19 @@ __global__ void __launch_bounds__(kAttendThreads, AttendCfg<FP8, DP, TMA>::CTAS)
             // the four warps' results meet: each in the stage that it has just used up
             float *mine = reinterpret_cast<float *>(smem + (warp * C::STAGES + stage) * C::STAGE_BYTES);
 #pragma unroll
-            for (int half = 0; half < 2; ++half) {
-                R.l[half] += __shfl_xor_sync(0xffffffffu, R.l[half], 1);
-                R.l[half] += __shfl_xor_sync(0xffffffffu, R.l[half], 2);
-                if (t == 0) {
-                    sh_m[warp][g + 8 * half] = R.m[half];
-                    sh_l[warp][g + 8 * half] = R.l[half];
+            for (int e = 0; e < 2; ++e) {
+#pragma unroll
+                for (int o = 4; o < 32; o <<= 1) R.l[e] += __shfl_xor_sync(0xffffffffu, R.l[e], o);
+                if (g == 0) {
+                    sh_m[warp][2 * t + e] = R.m[e];
+                    sh_l[warp][2 * t + e] = R.l[e];
                 }
             }
             const float back = FP8 ? R.vref * (1.f / kWeightUp) : 1.f;
 #pragma unroll
-            for (int i = 0; i < DP / 8; ++i)
+            for (int i = 0; i < DP / 16; ++i)
 #pragma unroll
-                for (int e = 0; e < 4; ++e)
-                    mine[(g + 8 * (e >> 1)) * DP + out_dim<FP8>(i, e, t)] = R.o[i][e] * back;
+                for (int e = 0; e < 4; ++e) mine[(2 * t + (e & 1)) * DP + out_dim<FP8>(i, e, g)] = R.o[i][e] * back;
             __syncthreads();
             const int item_first = comp.unit - comp.tile;   // unit of the item's first tile
             const bool whole = item_ends && item_first >= 0;
