@@ -386,7 +386,7 @@ __device__ __forceinline__ void rows_fetch(const RowsParams &R, RowsShared &sh, 
         const int h = a.k.h, page = id;
         at_next(P, a);
         id = look_up(a);
-#pragma unroll
+#pragma unroll 1
         for (int kv = 0; kv < 2; ++kv, ++unit) {
             const uint32_t stage = unit % RING;
             const uint32_t full = smem_addr(FP8 ? &sh.raw_full[stage] : &sh.full[stage]);
@@ -502,21 +502,17 @@ __device__ __forceinline__ void rows_convert(const RowsParams &R, RowsShared &sh
             if (!ok) continue;
             const uint8_t *src = smem_ptr + C::RAW_OFF + rs * C::RAW_BYTES;
             const uint32_t dst = smem + C::KV_OFF + st * C::TILE_BYTES;
-            uint4 x[STEPS];
-#pragma unroll
-            for (int i = 0; i < STEPS; ++i) x[i] = *reinterpret_cast<const uint4 *>(src + 16u * (tid + 128u * i));
-            mbar_arrive(smem_addr(&sh.raw_empty[rs]));
-#pragma unroll
+#pragma unroll 2
             for (int i = 0; i < STEPS; ++i) {
-                const uint32_t j = tid + 128u * i, r = j / CPR, c = j % CPR;
-                // lanes of the upper half of the dimensions, whose pieces lie in the same banks, store theirs the other way round
-                const bool swap = (c >> 2) & 1u;
-                const uint32_t lo[4] = {e4m3_to_f16(x[i].x), e4m3_to_f16_high(x[i].x), e4m3_to_f16(x[i].y), e4m3_to_f16_high(x[i].y)};
-                const uint32_t hi[4] = {e4m3_to_f16(x[i].z), e4m3_to_f16_high(x[i].z), e4m3_to_f16(x[i].w), e4m3_to_f16_high(x[i].w)};
-                const uint32_t first = dst + tc_piece(r, 2u * c + (swap ? 1u : 0u)), second = dst + tc_piece(r, 2u * c + (swap ? 0u : 1u));
-                sts16(first, swap ? hi[0] : lo[0], swap ? hi[1] : lo[1], swap ? hi[2] : lo[2], swap ? hi[3] : lo[3]);
-                sts16(second, swap ? lo[0] : hi[0], swap ? lo[1] : hi[1], swap ? lo[2] : hi[2], swap ? lo[3] : hi[3]);
+                // 8 lanes take the lower half of one row and the upper half of the next (then the other way round), so that neither
+                // their loads nor their stores meet in a bank
+                const uint32_t c = tid % CPR, pair = DP == 128 ? tid / 8u + 16u * (i >> 1) : 0u;
+                const uint32_t r = DP == 128 ? 2u * pair + ((c >> 2) ^ (i & 1u)) : (tid + 128u * i) / CPR;
+                const uint4 x = *reinterpret_cast<const uint4 *>(src + 16u * (r * CPR + c));
+                sts16(dst + tc_piece(r, 2u * c), e4m3_to_f16(x.x), e4m3_to_f16_high(x.x), e4m3_to_f16(x.y), e4m3_to_f16_high(x.y));
+                sts16(dst + tc_piece(r, 2u * c + 1u), e4m3_to_f16(x.z), e4m3_to_f16_high(x.z), e4m3_to_f16(x.w), e4m3_to_f16_high(x.w));
             }
+            mbar_arrive(smem_addr(&sh.raw_empty[rs]));
             fence_async_smem();
             mbar_arrive(smem_addr(&sh.full[st]));
         }
@@ -666,6 +662,7 @@ __device__ __forceinline__ void rows_mma(const RowsParams &R, RowsShared &sh, Ro
         for (int t = 0; t <= nt; ++t) {
             const uint32_t n = tile_no + t, u = 2u * n;  // K's place among the loaded tiles
             if (t > 0 && !wait(&sh.full[(u - 1u) % C::STAGES], ((u - 1u) / C::STAGES) & 1u, 0x812u)) return;
+#pragma unroll 1
             for (int i = 0; i < act; ++i) {
                 if (t > 0) {
                     if (!wait(&sh.p_half[i], p_phase[i] & 1u, 0x813u)) return;
@@ -942,24 +939,28 @@ struct RowState {
 
 // One tile of scores to weights, in tensor memory.  PLAIN (fp8): one scale, positive and finite, for every 8 tokens.
 //
-// Two passes over the scores, 32 at a time with the next 32 on their way: the maximum, then the weights.  Keeping all
-// 128 in registers saves the second read but unrolls the tile into more code than the instruction cache holds beside
-// the other roles' (fp8: 2.8 of 10 stall cycles per instruction were fetches).  The weights of the first two chunks lie in columns
-// of chunk 0, and so on: no score is overwritten before it has been read.
+// Two rolled passes over the scores, 32 at a time: the maximum, then the weights.  What bounds the softmax is fetching
+// instructions: five roles share the instruction cache, and every unrolled form loses more in fetches than it hides in
+// latencies (4,096-token chunk: all 128 scores in registers 1,241 us, 64 at a time with the next chunk on its way 1,246 us, this
+// 1,141 us).  For the same reason masks and scales per token, which few tiles have, are applied in the first pass and written
+// back.  The weights of two chunks take the columns of one chunk of scores that has been read.
 template <bool FP8, bool PLAIN, int DP>
 __device__ __forceinline__ void soft_tile(RowsShared &sh, RowState &S, uint32_t s_at, uint32_t o_at, uint32_t slot, int tok0, bool edge,
                                           bool first, float down_v, float scales, uint32_t half_bar, uint32_t full_bar, int lane)
 {
     using C = RowsCfg<FP8, DP>;
-    float2 a[16], b[16];
-    // the chunk's scores, scaled (one scale per token) and masked
-    auto settle = [&](float2 (&s)[16], int c) {
-        if (FP8 && !PLAIN) {
-            const float2 *ks = reinterpret_cast<const float2 *>(sh.ks[slot]) + 16 * c;
+    float2 s[16];
+    float top4[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+#pragma unroll 1
+    for (int c = 0; c < 4; ++c) {
+        tc_ld32(reinterpret_cast<uint32_t *>(s), s_at + 32u * c);
+        tc_wait_ld();
+        if (edge || !PLAIN) {
+            if (!PLAIN) {
+                const float2 *ks = reinterpret_cast<const float2 *>(sh.ks[slot]) + 16 * c;
 #pragma unroll
-            for (int e = 0; e < 16; ++e) s[e] = mul2(s[e], ks[e]);
-        }
-        if (edge) {
+                for (int e = 0; e < 16; ++e) s[e] = mul2(s[e], ks[e]);
+            }
             const int lo = S.lo - tok0 - 32 * c, hi = S.hi - tok0 - 32 * c;   // columns [lo, hi) count
             uint32_t seen = hi >= 32 ? 0xffffffffu : hi <= 0 ? 0u : (1u << hi) - 1u;
             seen &= lo <= 0 ? 0xffffffffu : lo >= 32 ? 0u : ~((1u << lo) - 1u);
@@ -968,11 +969,9 @@ __device__ __forceinline__ void soft_tile(RowsShared &sh, RowState &S, uint32_t 
                 if (!(seen & (1u << (2 * e)))) s[e].x = -INFINITY;
                 if (!(seen & (2u << (2 * e)))) s[e].y = -INFINITY;
             }
+            tc_st16(s_at + 32u * c, reinterpret_cast<const uint32_t *>(s));
+            tc_st16(s_at + 32u * c + 16u, reinterpret_cast<const uint32_t *>(s) + 16);
         }
-    };
-    float top4[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
-    auto largest = [&](float2 (&s)[16], int c) {
-        settle(s, c);
         if (!FP8 || !PLAIN) {
 #pragma unroll
             for (int e = 0; e < 16; ++e) top4[e & 3] = max3(top4[e & 3], s[e].x, s[e].y);
@@ -985,17 +984,8 @@ __device__ __forceinline__ void soft_tile(RowsShared &sh, RowState &S, uint32_t 
                 top4[g] = max2(top4[g], x == -INFINITY ? x : x * f);
             }
         }
-    };
-    tc_ld32(reinterpret_cast<uint32_t *>(a), s_at);
-#pragma unroll 1
-    for (int c = 0; c < 4; c += 2) {
-        tc_wait_ld();
-        tc_ld32(reinterpret_cast<uint32_t *>(b), s_at + 32u * (c + 1));
-        largest(a, c);
-        tc_wait_ld();
-        tc_ld32(reinterpret_cast<uint32_t *>(a), s_at + 32u * ((c + 2) & 3));   // in the end the first again
-        largest(b, c + 1);
     }
+    if (edge || !PLAIN) tc_wait_st();
     const float top = max2(max2(top4[0], top4[1]), max2(top4[2], top4[3]));
     const float x = top * S.mul;
     if (first) {
@@ -1019,8 +1009,10 @@ __device__ __forceinline__ void soft_tile(RowsShared &sh, RowState &S, uint32_t 
     }
     const float ref = S.m == -INFINITY ? 0.f : -S.m;
     const float2 ref_2 = make_float2(ref, ref);
-    auto weights = [&](float2 (&s)[16], int c) {
-        settle(s, c);
+#pragma unroll 1
+    for (int c = 0; c < 4; ++c) {
+        tc_ld32(reinterpret_cast<uint32_t *>(s), s_at + 32u * c);
+        tc_wait_ld();
         uint32_t pk[16];
         float2 mul_2 = make_float2(S.mul, S.mul);
         float fv = 1.f;
@@ -1032,7 +1024,7 @@ __device__ __forceinline__ void soft_tile(RowsShared &sh, RowState &S, uint32_t 
                 fv = __shfl_sync(0xffffffffu, scales, 16 + 4 * c + e / 4);
             }
             float2 y = fma2(s[e], mul_2, ref_2);
-            if ((e & 3) == 3) {
+            if ((e & 7) == 7) {   // one in eight: as much as pays beside the fetches of its code
                 y = poly_exp2(y);
             } else {
                 y.x = fast_exp2(y.x);
@@ -1054,19 +1046,12 @@ __device__ __forceinline__ void soft_tile(RowsShared &sh, RowState &S, uint32_t 
             }
         }
         tc_st16(s_at + 16u * c, pk);
-    };
-#pragma unroll 1
-    for (int c = 0; c < 4; c += 2) {
-        tc_wait_ld();
-        tc_ld32(reinterpret_cast<uint32_t *>(b), s_at + 32u * (c + 1));
-        weights(a, c);
-        tc_wait_ld();
-        if (c == 0) tc_ld32(reinterpret_cast<uint32_t *>(a), s_at + 64u);
-        weights(b, c + 1);
-        tc_wait_st();
-        tc_fence_before();
-        __syncwarp();
-        if (lane == 0) mbar_arrive(c == 0 ? half_bar : full_bar);
+        if (c & 1) {
+            tc_wait_st();
+            tc_fence_before();
+            __syncwarp();
+            if (lane == 0) mbar_arrive(c == 1 ? half_bar : full_bar);
+        }
     }
     if (!(top <= 3.402823466e38f)) S.sum[0].x = __int_as_float(0x7fc00000);   // a score of infinity or NaN: the row is no number
 }
@@ -1415,14 +1400,11 @@ __global__ void __launch_bounds__(kRowsThreads, 1) attend_rows_kernel(const __gr
 
     if (!any) {
     } else if (warp < 8) {
-        asm volatile("setmaxnreg.inc.sync.aligned.u32 200;");
         rows_softmax<FP8, DP>(R, sh, smem_ptr, smem, tmem, warp >> 2, tid);
     } else if (warp < 12) {
-        asm volatile("setmaxnreg.dec.sync.aligned.u32 64;");
         if (!R.tma) rows_load<FP8, DP>(R, sh, k, smem, tid - 256);
         else if (FP8) rows_convert<DP>(R, sh, k, smem_ptr, smem, tid - 256);
     } else {
-        asm volatile("setmaxnreg.dec.sync.aligned.u32 48;");
         if (warp == 12) {
             rows_mma<FP8, DP>(R, sh, k, __shfl_sync(0xffffffffu, smem, 0), __shfl_sync(0xffffffffu, tmem, 0));
             // whatever has been issued ends before the tensor memory is given back

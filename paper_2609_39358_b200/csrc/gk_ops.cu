@@ -216,10 +216,6 @@ int launch_rows(gk_ctx *c, const RowsParams &P, cudaStream_t st)
     using C = RowsCfg<FP8, DP>;
     static bool ready = false;
     if (!ready) {
-        cudaFuncAttributes a{};
-        GK_CUDA(c, cudaFuncGetAttributes(&a, attend_rows_kernel<FP8, DP>));
-        // the warp roles' shares of the registers add up to 128 a thread, which the launch has to bring along
-        if (a.numRegs < 128) return fail(c, GK_ERR_CUDA, "attend_rows_kernel was built with %d registers", a.numRegs);
         GK_CUDA(c, cudaFuncSetAttribute(attend_rows_kernel<FP8, DP>, cudaFuncAttributeMaxDynamicSharedMemorySize, C::SMEM));
         ready = true;
     }
