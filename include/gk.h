@@ -490,8 +490,11 @@ int gk_append(gk_ctx *ctx, const gk_cache *dst, uint32_t layer, const gk_batch *
  *
  * Scores, maxima, sums and outputs are accumulated in fp32; the bf16 result is rounded once.
  * The work is split along the cache among the whole GPU whatever the lengths; partial results are joined in a
- * fixed order, so a call with the same arguments gives the same bits.  Needs head_dim a multiple of 16 up
- * to 256 (else GK_ERR_UNSUPPORTED).  The first call of a context allocates its workspace (gk_stats.allocations; a call
+ * fixed order, so a call with the same arguments gives the same bits.  With more than 8 rows (max_q_len times the
+ * heads of a group; 32 with an fp8 cache) and head_dim up to 128 the weights are rounded to bf16 for a bf16 cache (to
+ * f16 for fp8) before they multiply V, else they keep 16 bits (11).  Needs head_dim a multiple of 16 up to 256 (else
+ * GK_ERR_UNSUPPORTED).  Should a wait inside a kernel run out (gk_stats.device_wait_expired), the results of that call must
+ * not be used, and gk_ctx_clear_error comes before the next one.  The first call of a context allocates its workspace (gk_stats.allocations; a call
  * with n_tokens == 0 does that and nothing else); later ones allocate nothing and may be captured.  */
 #define GK_ATTN_FULL 1u
 int gk_attention(gk_ctx *ctx, const gk_cache *cache, uint32_t layer, const gk_batch *batch, uint32_t q_heads,
