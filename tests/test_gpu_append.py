@@ -23,9 +23,14 @@ def table_of(R, far, seed=2):
 def reference(lay, p, layer, sq, k, v, rows, cos_sin, interleaved):
     """What the layer holds after the call, in 64 bits: [K, V] stored values, scales; and by how much each may differ."""
     kr = k.to(torch.float64) if cos_sin is None else rotate64(k, cos_sin, rows, interleaved)
-    slack_k = torch.zeros_like(kr) if cos_sin is None else 3 * 2.0 ** -24 * rotate64(
-        k.abs(), cos_sin.abs() * torch.cat([torch.ones(cos_sin.shape[1] // 2), -torch.ones(cos_sin.shape[1] // 2)]).cuda(),
-        rows, interleaved).abs() * 2
+    slack_k = torch.zeros_like(kr)
+    if cos_sin is not None:
+        # three roundings, each of at most 2^-24 of |a c| + |b s| (first of a pair) or |b c| + |a s| (second): with the
+        # sines' sign turned the first comes out as that sum, without it the second
+        size = cos_sin.abs()
+        minus = torch.cat([size[:, :size.shape[1] // 2], -size[:, size.shape[1] // 2:]], 1)
+        slack_k = 3 * 2.0 ** -24 * torch.maximum(rotate64(k.abs(), minus, rows, interleaved).abs(),
+                                                 rotate64(k.abs(), size, rows, interleaved).abs())
     new = [kr, v.to(torch.float64)]
     slack = [slack_k, torch.zeros_like(kr)]
     stored = [x.to(torch.float64).clone() for x in p.layer(layer)]
