@@ -9,7 +9,7 @@
 // Products.  mma.sync multiplies tiles of 16 x 16 with tiles of 16 x 8; the 16 rows are tokens (scores) and
 // dimensions (outputs) and the 8 columns are query rows, so that a group of up to 8 heads leaves nothing idle:
 //   S^T = K Q^T    (tokens x rows)        O^T += V^T P^T    (dimensions x rows)
-// tcgen05.mma has at least 64 rows on either side of K; a step has 8 query rows, and its products take a fifth of the
+// tcgen05.mma has at least 64 rows on either side of K; a step has 8 query rows, and its products take a tenth of the
 // time that its bytes do.
 //
 // Work.  An ITEM is (sequence, 8 query rows, key head); a query row is a (token, head of the group) pair, so
@@ -18,6 +18,10 @@
 // line.  No length, ragged or not, leaves a part of the GPU idle.  A CTA's stretch may begin and end inside an
 // item: the parts then go to the workspace, and the CTA that delivers an item's last part joins them in
 // the order of the line.
+//
+// Measured (one layer, 128 dimensions, back to back): 8 x 8,193 tokens, 8 key heads, bf16 (269 MB) 58 us, 4.6 TB/s, of which the
+// loop is 46 us; 32 x 2,100 tokens, 16 key heads, fp8 (276 MB) 63 us; one sequence of 97,561 tokens (400 MB) 77 us, 5.2
+// TB/s; 128 sequences of 18 to 9,001 tokens, 7 heads a group (387 MB) 82 us.
 //
 // A warp works alone: its own ring of stages filled by its own copies, its own running maximum, sum and output;
 // warps meet only at the end of an item.  Copies are tensor copies (TMA), one per page and 128 bytes of a row; where
