@@ -20,7 +20,7 @@
 //
 // Measured (32 query heads, 8 key heads, 128 dimensions, bf16): 4,096 tokens behind 16,384 (1.24 TFLOP) 1.12 ms cold, 1.10
 // PFLOP/s, and 1.30 ms back to back under the power cap; prompts of 700 to 5,200 tokens (255 GFLOP) 327 us; 61 tokens behind
-// 97,560 in 8 bits (98 GFLOP, 201 MB) 194 us, bound by instructions: conversion and softmax share the schedulers.
+// 97,560 in 8 bits (98 GFLOP, 201 MB) 167 us, bound by instructions: conversion and softmax share the schedulers.
 // Scores read Q and K at the full 128 bytes a cycle of shared memory, so that V, the copies and the conversion wait for them;
 // and a tile's next scores wait for its weights' product, in whose place they go.
 //
@@ -904,25 +904,27 @@ __device__ __forceinline__ void add_not_finite(const AttendParams &P, const Rows
     }
 }
 
-// One row's parts in the order of the line: 32 outputs from d on, and the row's maximum and sum.
-template <int DP>
-__device__ __forceinline__ void join_row(const float *parts, uint32_t c0, uint32_t c1, int prow, int d, float (&v)[32], float &m, float &l)
+// One row's parts in the order of the line: N outputs from d on, and the row's maximum and sum.
+// Parts are loaded U at a time.
+template <int DP, int U, int N>
+__device__ __forceinline__ void join_row(const float *parts, uint32_t c0, uint32_t c1, int prow, int d, float (&v)[N], float &m, float &l)
 {
     constexpr size_t PF = (size_t)kRowsBlock * (DP + 2);
     m = -INFINITY;
+#pragma unroll 8
     for (uint32_t c = c0; c <= c1; ++c)
         m = fmaxf(m, __ldcg(parts + (2u * c + (c == c0 ? 1u : 0u)) * PF + kRowsBlock * DP + prow));
     const float ref = m == -INFINITY ? 0.f : m;
     l = 0.f;
 #pragma unroll
-    for (int e = 0; e < 32; ++e) v[e] = 0.f;
-#pragma unroll 2
+    for (int e = 0; e < N; ++e) v[e] = 0.f;
+#pragma unroll U
     for (uint32_t c = c0; c <= c1; ++c) {
         const float *p = parts + (2u * c + (c == c0 ? 1u : 0u)) * PF;
         const float f = fast_exp2(__ldcg(p + kRowsBlock * DP + prow) - ref);
         l += f * __ldcg(p + kRowsBlock * (DP + 1) + prow);
 #pragma unroll
-        for (int e = 0; e < 8; ++e) {
+        for (int e = 0; e < N / 4; ++e) {
             const float4 y = __ldcg(reinterpret_cast<const float4 *>(p + (size_t)((d / 4 + e) * kRowsBlock + prow) * 4));
             v[4 * e] += f * y.x;
             v[4 * e + 1] += f * y.y;
@@ -1239,7 +1241,7 @@ __device__ __forceinline__ void rows_softmax(const RowsParams &R, RowsShared &sh
 #pragma unroll 1
                     for (int d = 0; d < (int)P.cache.D; d += 32) {
                         float v[32];
-                        join_row<DP>(P.parts, w.c0, w.c1, live ? prow : 0, d, v, jm, jl);
+                        join_row<DP, 2, 32>(P.parts, w.c0, w.c1, live ? prow : 0, d, v, jm, jl);
                         __syncwarp();
                         store_rows(P, out, live, d, v, jl == 0.f ? 0.f : 1.f / jl, lane);
                     }
@@ -1253,25 +1255,27 @@ __device__ __forceinline__ void rows_softmax(const RowsParams &R, RowsShared &sh
     }
 }
 
-// Blocks that many CTAs share: 32 rows and 32 outputs of each a warp.
+// Blocks that many CTAs share: 32 rows and 8 outputs of each a warp, so that a few blocks fill the GPU with loads (8 blocks of
+// 19 parts, 19 MB from a cold cache: 18 us; with 32 outputs a warp and two parts at a time 47 us).
 template <int DP>
-__global__ void __launch_bounds__(128) join_rows_kernel(const __grid_constant__ RowsParams R)
+__global__ void __launch_bounds__(DP * 4) join_rows_kernel(const __grid_constant__ RowsParams R)
 {
     const AttendParams &P = R.a;
     grid_begin();
     const RowsJoin j = R.join[blockIdx.x];
-    const int d = 32 * (threadIdx.x >> 5), prow = (int)blockIdx.y * 32 + (threadIdx.x & 31);
+    const int d = 8 * (threadIdx.x >> 5), prow = (int)blockIdx.y * 32 + (threadIdx.x & 31);
     if (j.parts == 0 || d >= (int)P.cache.D) return;
     const RowsSeq w = rows_seq(P, j.s);
     const int row = j.blk * kRowsBlock + prow;
-    const bool live = row < w.q_len * (int)P.G;
-    if (!__any_sync(0xffffffffu, live)) return;
-    float v[32], m, l;
-    join_row<DP>(P.parts, blockIdx.x, blockIdx.x + j.parts - 1u, live ? prow : 0, d, v, m, l);
+    if (row >= w.q_len * (int)P.G) return;
+    float v[8], m, l;
+    join_row<DP, 8, 8>(P.parts, blockIdx.x, blockIdx.x + j.parts - 1u, prow, d, v, m, l);
     uint64_t lse_at;
-    __nv_bfloat16 *out = row_out(P, w.q0, j.h, live ? row : 0, lse_at);
-    store_rows(P, out, live, d, v, l == 0.f ? 0.f : 1.f / l, threadIdx.x & 31);
-    if (P.lse && d == 0 && live) P.lse[lse_at] = lse_of(m, l);
+    __nv_bfloat16 *out = row_out(P, w.q0, j.h, row, lse_at);
+    const float f = l == 0.f ? 0.f : 1.f / l;
+    *reinterpret_cast<uint4 *>(out + d) = make_uint4(bf16x2(v[0] * f, v[1] * f), bf16x2(v[2] * f, v[3] * f), bf16x2(v[4] * f, v[5] * f),
+                                                     bf16x2(v[6] * f, v[7] * f));
+    if (P.lse && d == 0) P.lse[lse_at] = lse_of(m, l);
 }
 
 template <bool FP8, int DP>

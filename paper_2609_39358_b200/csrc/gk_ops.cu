@@ -220,7 +220,7 @@ int launch_rows(gk_ctx *c, const RowsParams &P, cudaStream_t st)
         ready = true;
     }
     int rc = launch(c, false, attend_rows_kernel<FP8, DP>, dim3(c->sm_count), kRowsThreads, C::SMEM, st, P);
-    if (rc == GK_OK && P.join) rc = launch(c, true, join_rows_kernel<DP>, dim3(c->sm_count, kRowsBlock / 32), DP, 0, st, P);
+    if (rc == GK_OK && P.join) rc = launch(c, true, join_rows_kernel<DP>, dim3(c->sm_count, kRowsBlock / 32), DP * 4, 0, st, P);
     return rc;
 }
 
